@@ -272,6 +272,123 @@ int cluster_attention_fwd_static(const ca_problem_t* p, const void* Qp, const vo
                                  const int32_t* perm_q, void* O, float* lse, void* stream);
 int ca_static_last_status(void);
 
+/*
+ * Attention over streams of tokens: rotary positions, a cache in pages, one new token against it, and
+ * attention over a sliding window.  (The paper's models rotate queries and keys before any attention and
+ * its method takes the keys of a whole sequence; these calls are what a stream of frames or tokens needs
+ * next to it.)
+ *
+ * Tensors of these calls are [batch, heads, rows, head_dim] by strides, so that a projection's output (rows
+ * before heads) is taken as it is.  Strides are in elements, the last dimension is dense, data is 16-byte
+ * aligned and every stride is a multiple of 16 bytes (the stride of a dimension of extent 1 is not looked
+ * at); rows of outputs do not overlap (strides of at least head_dim).  head_dim is 64 or 128.  Several query
+ * heads may share a key head: heads_q is a multiple of heads_kv, query head h reads key head
+ * h / (heads_q / heads_kv).
+ */
+typedef struct {
+  void* data;
+  int64_t stride_b, stride_h, stride_n;
+} ca_rows_t;
+
+/*
+ * Rotary positions.  A position has 1 to 4 axes (time, height, width); pairs[a] pairs of channels turn with
+ * axis a, the axes' pairs one after the other, head_dim/2 in all at most; channels behind the last pair stay as
+ * they are.  Pair c is channels (2c, 2c + 1) if `adjacent`, else (c, R + c) with R the number of all pairs.
+ *   t = position[axis of c] * freq[c];  (x, y) -> (x cos t - y sin t, x sin t + y cos t)
+ * Positions are whole numbers of any size and sign; t is reduced exactly, sine and cosine and the
+ * rotation are float32, the result is rounded once.
+ */
+typedef struct {
+  int32_t axes;
+  int32_t pairs[4];
+  int32_t adjacent;
+  const double* freq;      /* HOST pointer: radians per step of each pair, at most 2^32 in magnitude */
+} ca_rotary_t;
+
+/*
+ * Q, K -> Qo, Ko with `n` rows at `positions` [batch, n, axes] int32 (device; batch items pos_stride_b
+ * apart, 0: the same for all).  inverse != 0 turns by -t: the transpose, which carries gradients of the
+ * rotated rows back.  heads_k may be 0 (K, Ko NULL).  An output may be its input, with the same strides.
+ * No workspace.
+ */
+int rotary_axes(const ca_rotary_t* rot, int32_t batch, int32_t heads_q, int32_t heads_k, int32_t n,
+                int32_t head_dim, int32_t dtype, int32_t inverse, const ca_rows_t* Q, const ca_rows_t* K,
+                const int32_t* positions, int64_t pos_stride_b, const ca_rows_t* Qo, const ca_rows_t* Ko,
+                void* stream);
+
+/*
+ * A cache in pages.  K_pages, V_pages: pools [pages, heads_kv, page_rows, head_dim], dense.  Row j of
+ * sequence b stands in page page_table[b, j / page_rows] at place j % page_rows.  Entries of the table and places
+ * that hold no row of a sequence may be anything.
+ */
+typedef struct {
+  int32_t batch, heads_q, heads_kv;
+  int32_t head_dim, dtype;
+  int32_t page_rows;            /* 16 .. 1024, any number */
+  int32_t pages;                /* of a pool */
+  int32_t pages_per_sequence;   /* entries of a row of page_table */
+  int32_t left;                 /* attention: rows before the new one that stay visible; -1: all */
+  int32_t sinks;                /* attention: first rows that stay visible beside the window */
+  float softmax_scale;          /* 0 selects 1/sqrt(head_dim) */
+} ca_cache_t;
+
+/* Bytes of workspace of the two calls below (one workspace serves both, one call at a time). */
+int ca_cache_workspace_bytes(const ca_cache_t* c, size_t* bytes);
+
+/*
+ * Puts n new rows of every sequence behind the lengths[b] rows that are there: rows i < count[b] (count
+ * NULL: all n) of K and V [batch, heads_kv, n, head_dim] go to rows lengths[b] + i.  K is turned by `rot` at
+ * `positions` on the way (rot NULL: as it is).  lengths [batch], count [batch], page_table
+ * [batch, pages_per_sequence] int32 (device) are only read.  A page that rows are put into belongs to one
+ * sequence.  A row whose place is out of range (a page that the pool or the table does not have, a negative length, a
+ * count that is not in 0 .. n) is left out and CA_ERR_BAD_INDEX recorded.
+ */
+int cache_append(const ca_cache_t* c, int32_t n, const ca_rows_t* K, const ca_rows_t* V,
+                 const int32_t* lengths, const int32_t* count, const int32_t* page_table,
+                 const ca_rotary_t* rot, const int32_t* positions, int64_t pos_stride_b, void* K_pages,
+                 void* V_pages, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * Attention of one new token per sequence: Q [batch, heads_q, 1, head_dim] against the first
+ * N = lengths[b] + appended rows of sequence b (`appended`: rows put there since lengths was written; the
+ * token's own key is among the N rows), of which
+ *   j >= N - 1 - left   or   j < sinks
+ * are visible.  O [batch, heads_q, 1, head_dim] = softmax-weighted mean of their values, lse
+ * [batch, heads_q] fp32 or NULL = log-sum-exp of their logits; without a visible row zeros and -inf.
+ * What is not visible is not read.  A length out of range is cut to the range, a page out of range read as zero
+ * keys and values, and CA_ERR_BAD_INDEX recorded.  The result does not depend on how the GPU schedules the parts.
+ */
+int paged_attention_fwd(const ca_cache_t* c, const ca_rows_t* Q, const void* K_pages, const void* V_pages,
+                        const int32_t* lengths, int32_t appended, const int32_t* page_table,
+                        const ca_rows_t* O, float* lse, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * Attention over a sliding window with first tokens that stay visible.  Batch item b has len_q[b] query
+ * rows and len_k[b] key rows (int32, device; NULL: n_q, n_k for all), the last query stands at the last key:
+ * query i at p = i + len_k - len_q.  It sees key j if
+ *   j <= p + right   and   (j >= p - left   or   j < sinks);         a bound of -1 is none
+ * (right = 0: causal; first tokens that stand behind p + right are not seen).  O = softmax-weighted mean of
+ * the visible values, lse [batch, heads_q, n_q] fp32 or NULL; a row that sees nothing: zeros and -inf.  Rows from
+ * len_q[b] on are left as they were, in O and lse, and rows of K and V from len_k[b] on are not used.
+ * bf16 storage runs on tcgen05 tensor cores with fp32 accumulation and bf16 probabilities (CA_ATTN_FP32 in
+ * flags, or fp32 storage: the FP32 CUDA-core kernel).  A length out of range is cut to it and
+ * CA_ERR_BAD_INDEX recorded.
+ */
+typedef struct {
+  int32_t batch, heads_q, heads_kv;
+  int32_t n_q, n_k;
+  int32_t head_dim, dtype;
+  int32_t left, right;          /* -1, or 0 and more */
+  int32_t sinks;
+  float softmax_scale;          /* 0 selects 1/sqrt(head_dim) */
+  int32_t flags;                /* CA_ATTN_FP32 or 0 */
+} ca_window_t;
+
+int ca_window_workspace_bytes(const ca_window_t* p, size_t* bytes);
+int window_attention_fwd(const ca_window_t* p, const ca_rows_t* Q, const ca_rows_t* K, const ca_rows_t* V,
+                         const int32_t* len_q, const int32_t* len_k, const ca_rows_t* O, float* lse,
+                         void* ws, size_t ws_bytes, void* stream);
+
 /* Reads the status word of a workspace as the last call on it left it (synchronises the device). */
 int ca_last_status(const void* ws);
 

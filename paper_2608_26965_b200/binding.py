@@ -30,7 +30,8 @@ EXPORTS = ("ca_workspace_bytes", "cluster_qk", "select_blocks", "cluster_attenti
            "ca_last_status", "ca_attn_recomputed", "ca_version", "ca_kernel_launches", "cluster_attention_fwd_static",
            "ca_static_scratch_bytes", "ca_static_last_status", "select_blocks_adaptive",
            "cluster_attention_fwd_ragged", "ca_basic_workspace_bytes", "cluster_qk_basic", "ca_debug_attn_wait", "ca_debug_eigh",
-           "ca_profile", "ca_profile_read")
+           "ca_profile", "ca_profile_read", "rotary_axes", "ca_cache_workspace_bytes", "cache_append",
+           "paged_attention_fwd", "ca_window_workspace_bytes", "window_attention_fwd")
 
 
 class CaProblem(ctypes.Structure):
@@ -52,6 +53,30 @@ class CaProblem(ctypes.Structure):
         vals = {f: getattr(self, f) for f, _ in self._fields_}
         vals.update(kw)
         return CaProblem(**vals)
+
+
+class CaRows(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("stride_b", ctypes.c_int64), ("stride_h", ctypes.c_int64),
+                ("stride_n", ctypes.c_int64)]
+
+
+class CaRotary(ctypes.Structure):
+    _fields_ = [("axes", ctypes.c_int32), ("pairs", ctypes.c_int32 * 4), ("adjacent", ctypes.c_int32),
+                ("freq", ctypes.POINTER(ctypes.c_double))]
+
+
+class CaCache(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("heads_q", ctypes.c_int32), ("heads_kv", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("dtype", ctypes.c_int32), ("page_rows", ctypes.c_int32),
+                ("pages", ctypes.c_int32), ("pages_per_sequence", ctypes.c_int32), ("left", ctypes.c_int32),
+                ("sinks", ctypes.c_int32), ("softmax_scale", ctypes.c_float)]
+
+
+class CaWindow(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("heads_q", ctypes.c_int32), ("heads_kv", ctypes.c_int32),
+                ("n_q", ctypes.c_int32), ("n_k", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("left", ctypes.c_int32), ("right", ctypes.c_int32),
+                ("sinks", ctypes.c_int32), ("softmax_scale", ctypes.c_float), ("flags", ctypes.c_int32)]
 
 
 class ClusterAttnError(RuntimeError):
@@ -114,6 +139,19 @@ def load_library() -> ctypes.CDLL:
     lib.ca_profile_read.argtypes = [ctypes.c_int, ctypes.POINTER(ctypes.c_char_p), ctypes.POINTER(ctypes.c_float),
                                     ctypes.POINTER(ctypes.c_int)]
     lib.ca_profile_read.restype = ctypes.c_int
+    i32, i64, rp = ctypes.c_int32, ctypes.c_int64, ctypes.POINTER(CaRows)
+    lib.rotary_axes.argtypes = [ctypes.POINTER(CaRotary)] + [i32] * 7 + [rp, rp, vp, i64, rp, rp, vp]
+    lib.rotary_axes.restype = ctypes.c_int
+    lib.ca_cache_workspace_bytes.argtypes = [ctypes.POINTER(CaCache), ctypes.POINTER(sz)]
+    lib.ca_cache_workspace_bytes.restype = ctypes.c_int
+    lib.cache_append.argtypes = [ctypes.POINTER(CaCache), i32, rp, rp, vp, vp, vp, ctypes.POINTER(CaRotary), vp, i64, vp, vp, vp, sz, vp]
+    lib.cache_append.restype = ctypes.c_int
+    lib.paged_attention_fwd.argtypes = [ctypes.POINTER(CaCache), rp, vp, vp, vp, i32, vp, rp, vp, vp, sz, vp]
+    lib.paged_attention_fwd.restype = ctypes.c_int
+    lib.ca_window_workspace_bytes.argtypes = [ctypes.POINTER(CaWindow), ctypes.POINTER(sz)]
+    lib.ca_window_workspace_bytes.restype = ctypes.c_int
+    lib.window_attention_fwd.argtypes = [ctypes.POINTER(CaWindow), rp, rp, rp, vp, vp, rp, vp, vp, sz, vp]
+    lib.window_attention_fwd.restype = ctypes.c_int
     _lib = lib
     return lib
 
@@ -366,13 +404,32 @@ class Plan:
         _check(rc, "cluster_attention_fwd_ragged")
         return self.O, (self.lse if want_lse else None)
 
-    def forward_adaptive(self, Q, K, V, recall: float, min_count: int = 16, want_lse=False, stream=None):
+    def _turned(self, Q, K, rotary, positions_q, positions_k, stream):
+        """Q and K turned by their positions (rotary_axes), in buffers of the plan."""
+        p, dt = self.problem, torch_dtype(self.problem)
+        if getattr(self, "Qr", None) is None:
+            self.Qr = torch.empty((p.batch, p.heads, p.n_q, p.head_dim), dtype=dt, device=self.device)
+            self.Kr = torch.empty((p.batch, p.heads, p.n_k, p.head_dim), dtype=dt, device=self.device)
+        if positions_k is None and p.n_q == p.n_k:
+            return rotary_axes(rotary, Q, K, positions_q, out_q=self.Qr, out_k=self.Kr, stream=stream)
+        rotary_axes(rotary, Q, None, positions_q, out_q=self.Qr, stream=stream)
+        rotary_axes(rotary, K, None, positions_k, out_q=self.Kr, stream=stream)
+        return self.Qr, self.Kr
+
+    def forward_adaptive(self, Q, K, V, recall: float, min_count: int = 16, want_lse=False, stream=None, rotary=None,
+                         positions_q=None, positions_k=None):
+        if rotary is not None:
+            Q, K = self._turned(Q, K, rotary, positions_q, positions_k, stream)
         self.cluster_qk(Q, K, V, stream=stream)
         self.select_blocks_adaptive(recall, min_count, stream=stream)
         return self.cluster_attention_fwd_ragged(want_lse=want_lse, stream=stream)
 
-    def forward(self, Q, K, V, want_lse=False, stream=None):
-        """The whole hot path: clustering, block selection, attention."""
+    def forward(self, Q, K, V, want_lse=False, stream=None, rotary=None, positions_q=None, positions_k=None):
+        """The whole hot path: clustering, block selection, attention.  With `rotary` (a Rotary) the queries and
+        keys are turned first, by positions_q and positions_k [batch or 1, n, axes] int32 (positions_k None: the
+        queries' own); Q and K may then be strided."""
+        if rotary is not None:
+            Q, K = self._turned(Q, K, rotary, positions_q, positions_k, stream)
         self.cluster_qk(Q, K, V, stream=stream)
         self.select_blocks(stream=stream)
         return self.cluster_attention_fwd(want_lse=want_lse, stream=stream)[0]
@@ -389,6 +446,250 @@ class Plan:
         if n < 0:
             _check(-n, "ca_attn_recomputed")
         return n
+
+
+# -- streams of tokens: rotary positions, a cache in pages, sliding windows -----------
+# These calls take [batch, heads, rows, head_dim] tensors by strides (the last dimension dense, strides of
+# 16 bytes), run on the device of their tensors whatever the current one is, and by default on its current stream.
+_CODES = {"fp32": CA_DTYPE_FP32, "bf16": CA_DTYPE_BF16}
+_TORCH = {CA_DTYPE_FP32: torch.float32, CA_DTYPE_BF16: torch.bfloat16}
+_OF_TORCH = {torch.float32: CA_DTYPE_FP32, torch.bfloat16: CA_DTYPE_BF16}
+
+
+def _code(dtype: str) -> int:
+    if dtype not in _CODES:
+        raise ClusterAttnError(f"dtype must be one of {sorted(_CODES)}, not {dtype!r}")
+    return _CODES[dtype]
+
+
+def _rows(t: torch.Tensor, name: str, shape, dtype: torch.dtype, device: torch.device) -> CaRows:
+    """A [batch, heads, rows, head_dim] tensor of that shape, type and device as the library takes it."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise ClusterAttnError(f"{name} must be a CUDA tensor (no CPU path exists)")
+    if t.device != device:
+        raise ClusterAttnError(f"{name} is on {t.device}, the call on {device}")
+    if t.dtype != dtype:
+        raise ClusterAttnError(f"{name} must be {dtype}, not {t.dtype}")
+    if tuple(t.shape) != tuple(shape):
+        raise ClusterAttnError(f"{name} must be {list(shape)}, not {list(t.shape)}")
+    sb, sh, sn, sd = t.stride()
+    if sd != 1:
+        raise ClusterAttnError(f"{name}: the last dimension must be dense")
+    return CaRows(t.data_ptr(), sb, sh, sn)
+
+
+def _int32(t: Optional[torch.Tensor], name: str, shape, device: torch.device):
+    """A dense int32 tensor of that shape, or None."""
+    if t is None:
+        return None
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.device != device:
+        raise ClusterAttnError(f"{name} must be a CUDA tensor on {device}")
+    if t.dtype != torch.int32 or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+        raise ClusterAttnError(f"{name} must be a contiguous int32 tensor {list(shape)}, not {t.dtype} {list(t.shape)}")
+    return ctypes.c_void_p(t.data_ptr())
+
+
+def _cuda_device(device) -> torch.device:
+    d = torch.device(device)
+    if d.type != "cuda" or not torch.cuda.is_available():
+        raise ClusterAttnError("no CUDA device: libclusterattn has no CPU path")
+    return d if d.index is not None else torch.device("cuda", torch.cuda.current_device())
+
+
+def _call(fn, what: str, device: torch.device, stream: Optional[torch.cuda.Stream], *args) -> None:
+    """A library call on `stream` (default: the device's current one) with the device current."""
+    if stream is not None and stream.device != device:
+        raise ClusterAttnError(f"{what}: the stream is on {stream.device}, the tensors on {device}")
+    handle = ctypes.c_void_p((stream if stream is not None else torch.cuda.current_stream(device)).cuda_stream)
+    if torch.cuda.current_device() == device.index:
+        rc = fn(*args, handle)
+    else:
+        with torch.cuda.device(device):
+            rc = fn(*args, handle)
+    _check(rc, what)
+
+
+class Rotary:
+    """Rotary positions: pairs[a] pairs of channels turn with axis a of a position, by `frequencies` (radians
+    per step, one for every pair), or theta ** (-i / pairs[a]) for pair i of an axis.  adjacent: pair c is
+    channels (2c, 2c + 1), otherwise (c, R + c) with R the number of pairs."""
+
+    def __init__(self, head_dim: int, pairs, theta: float = 10000.0, frequencies=None, adjacent: bool = True):
+        pairs = [int(p) for p in pairs]
+        if not 1 <= len(pairs) <= 4 or min(pairs) < 0 or not 1 <= sum(pairs) <= head_dim // 2:
+            raise ClusterAttnError(f"pairs must be 1 to 4 counts, 1 to {head_dim // 2} in all, not {pairs}")
+        if frequencies is None:
+            frequencies = [theta ** (-i / n) for n in pairs for i in range(n)]
+        frequencies = [float(f) for f in frequencies]
+        if len(frequencies) != sum(pairs) or not all(abs(f) <= 2.0 ** 32 for f in frequencies):
+            raise ClusterAttnError(f"frequencies must be {sum(pairs)} numbers of at most 2^32")
+        self.head_dim, self.pairs, self.frequencies, self.adjacent = int(head_dim), pairs, frequencies, bool(adjacent)
+        self._freq = (ctypes.c_double * len(frequencies))(*frequencies)
+        self._struct = CaRotary(len(pairs), (ctypes.c_int32 * 4)(*pairs), 1 if adjacent else 0,
+                                ctypes.cast(self._freq, ctypes.POINTER(ctypes.c_double)))
+
+    def _positions(self, positions, batch: int, n: int, device: torch.device):
+        """Pointer and batch stride of positions [batch, n, axes], or [1, n, axes] for the whole batch."""
+        axes = len(self.pairs)
+        shape = (1 if isinstance(positions, torch.Tensor) and positions.dim() == 3 and positions.shape[0] == 1 else batch, n, axes)
+        if positions is None:
+            raise ClusterAttnError("positions are missing")
+        return _int32(positions, "positions", shape, device), (0 if shape[0] == 1 else n * axes)
+
+
+def rotary_axes(rotary: Rotary, q, k, positions, inverse: bool = False, out_q=None, out_k=None, stream=None):
+    """rotary_axes of the C library: q [batch, heads, n, head_dim] and k (or None) turned by their positions
+    [batch or 1, n, axes] int32.  Returns (q', k'): new dense tensors, or out_q / out_k, which may be q and k."""
+    if not isinstance(q, torch.Tensor) or q.dim() != 4 or q.dtype not in _OF_TORCH:
+        raise ClusterAttnError("q must be a [batch, heads, n, head_dim] tensor of float32 or bfloat16")
+    device = _cuda_device(q.device)
+    B, H, n, D = q.shape
+    if D != rotary.head_dim:
+        raise ClusterAttnError(f"q has head_dim {D}, the rotary positions {rotary.head_dim}")
+    if k is None and out_k is not None:
+        raise ClusterAttnError("out_k without k")
+    Hk = 0
+    if k is not None:
+        if not isinstance(k, torch.Tensor) or k.dim() != 4:
+            raise ClusterAttnError("k must be a [batch, heads, n, head_dim] tensor")
+        Hk = k.shape[1]
+    pos, pos_b = rotary._positions(positions, B, n, device)
+    if out_q is None or (k is not None and out_k is None):
+        with torch.cuda.stream(stream):                    # new memory is in order with what the call's stream does (None: no change)
+            out_q = torch.empty((B, H, n, D), dtype=q.dtype, device=device) if out_q is None else out_q
+            out_k = torch.empty((B, Hk, n, D), dtype=q.dtype, device=device) if k is not None and out_k is None else out_k
+    a, c = _rows(q, "q", (B, H, n, D), q.dtype, device), _rows(out_q, "out_q", (B, H, n, D), q.dtype, device)
+    b = d = None
+    if k is not None:
+        b, d = _rows(k, "k", (B, Hk, n, D), q.dtype, device), _rows(out_k, "out_k", (B, Hk, n, D), q.dtype, device)
+    _call(load_library().rotary_axes, "rotary_axes", device, stream, rotary._struct, B, H, Hk, n, D, _OF_TORCH[q.dtype],
+          1 if inverse else 0, a, b, pos, pos_b, c, d)
+    return out_q, out_k
+
+
+def make_cache_problem(batch: int, heads_q: int, heads_kv: int, head_dim: int, dtype: str, page_rows: int, pages: int,
+                       pages_per_sequence: int, left: int = -1, sinks: int = 0, softmax_scale: float = 0.0) -> CaCache:
+    return CaCache(batch, heads_q, heads_kv, head_dim, _code(dtype), page_rows, pages, pages_per_sequence, left, sinks,
+                   float(softmax_scale))
+
+
+class PagedCache:
+    """Keys and values of `batch` sequences in pages: pools K_pages, V_pages [pages, heads_kv, page_rows, head_dim],
+    page_table [batch, pages_per_sequence] and lengths [batch] int32 (made here, zeros, where they are not given), and the
+    workspace and outputs of the calls.  The program that owns the cache writes page_table and lengths; the
+    calls only read them."""
+
+    def __init__(self, problem: CaCache, device: str = "cuda:0", K_pages=None, V_pages=None, page_table=None, lengths=None):
+        self.device = dev = _cuda_device(device)
+        self.problem = p = problem
+        lib = load_library()
+        size = ctypes.c_size_t()
+        _check(lib.ca_cache_workspace_bytes(ctypes.byref(p), ctypes.byref(size)), "ca_cache_workspace_bytes")
+        self.dtype = _TORCH[p.dtype]
+        pool = (p.pages, p.heads_kv, p.page_rows, p.head_dim)
+        self.K_pages = torch.zeros(pool, dtype=self.dtype, device=dev) if K_pages is None else K_pages
+        self.V_pages = torch.zeros(pool, dtype=self.dtype, device=dev) if V_pages is None else V_pages
+        self.page_table = (torch.zeros((p.batch, p.pages_per_sequence), dtype=torch.int32, device=dev)
+                           if page_table is None else page_table)
+        self.lengths = torch.zeros((p.batch,), dtype=torch.int32, device=dev) if lengths is None else lengths
+        self._pools()
+        self._indices()
+        self.O = torch.zeros((p.batch, p.heads_q, 1, p.head_dim), dtype=self.dtype, device=dev)
+        self.lse = torch.zeros((p.batch, p.heads_q, 1), dtype=torch.float32, device=dev)
+        self.ws = torch.zeros(size.value, dtype=torch.uint8, device=dev)
+
+    def _pools(self):
+        p = self.problem
+        for name, t in (("K_pages", self.K_pages), ("V_pages", self.V_pages)):
+            _rows(t, name, (p.pages, p.heads_kv, p.page_rows, p.head_dim), self.dtype, self.device)
+            if not t.is_contiguous():
+                raise ClusterAttnError(f"{name} must be contiguous")
+        return _ptr(self.K_pages), _ptr(self.V_pages)
+
+    def _indices(self):
+        p = self.problem
+        return (_int32(self.lengths, "lengths", (p.batch,), self.device),
+                _int32(self.page_table, "page_table", (p.batch, p.pages_per_sequence), self.device))
+
+    def cache_append(self, K, V, count=None, rotary: Optional[Rotary] = None, positions=None, stream=None):
+        """cache_append of the C library: rows of K and V [batch, heads_kv, n, head_dim] (of sequence b the first
+        count[b]) behind the lengths[b] rows that are there, K turned by `rotary` at `positions` on the way."""
+        p = self.problem
+        if not isinstance(K, torch.Tensor) or K.dim() != 4:
+            raise ClusterAttnError("K must be a [batch, heads_kv, n, head_dim] tensor")
+        n = K.shape[2]
+        shape = (p.batch, p.heads_kv, n, p.head_dim)
+        k, v = _rows(K, "K", shape, self.dtype, self.device), _rows(V, "V", shape, self.dtype, self.device)
+        pos, pos_b, rot = None, 0, None
+        if rotary is not None:
+            if rotary.head_dim != p.head_dim:
+                raise ClusterAttnError(f"the cache has head_dim {p.head_dim}, the rotary positions {rotary.head_dim}")
+            pos, pos_b = rotary._positions(positions, p.batch, n, self.device)
+            rot = rotary._struct
+        elif positions is not None:
+            raise ClusterAttnError("positions without rotary")
+        lengths, table = self._indices()
+        kp, vp = self._pools()
+        _call(load_library().cache_append, "cache_append", self.device, stream, p, n, k, v, lengths,
+              _int32(count, "count", (p.batch,), self.device), table, rot, pos, pos_b, kp, vp, _ptr(self.ws), self.ws.numel())
+
+    def paged_attention_fwd(self, Q, appended: int = 0, out=None, want_lse: bool = True, stream=None):
+        """paged_attention_fwd of the C library: Q [batch, heads_q, 1, head_dim] against lengths[b] + appended
+        rows.  Returns (O, lse [batch, heads_q, 1] or None): the cache's buffers, O or `out`."""
+        p = self.problem
+        shape = (p.batch, p.heads_q, 1, p.head_dim)
+        out = self.O if out is None else out
+        q, o = _rows(Q, "Q", shape, self.dtype, self.device), _rows(out, "out", shape, self.dtype, self.device)
+        lengths, table = self._indices()
+        kp, vp = self._pools()
+        lse = self.lse if want_lse else None
+        _call(load_library().paged_attention_fwd, "paged_attention_fwd", self.device, stream, p, q, kp, vp, lengths,
+              int(appended), table, o, _ptr(lse), _ptr(self.ws), self.ws.numel())
+        return out, lse
+
+    def last_status(self) -> int:
+        """Status word that the last call left (ca_last_status; synchronises the device)."""
+        with torch.cuda.device(self.device):
+            return load_library().ca_last_status(_ptr(self.ws))
+
+
+def make_window_problem(batch: int, heads_q: int, heads_kv: int, n_q: int, n_k: int, head_dim: int, dtype: str, left: int,
+                        right: int, sinks: int = 0, softmax_scale: float = 0.0, flags: int = 0) -> CaWindow:
+    return CaWindow(batch, heads_q, heads_kv, n_q, n_k, head_dim, _code(dtype), left, right, sinks, float(softmax_scale), flags)
+
+
+class WindowPlan:
+    """Outputs and workspace of attention over a sliding window for one problem shape."""
+
+    def __init__(self, problem: CaWindow, device: str = "cuda:0"):
+        self.device = dev = _cuda_device(device)
+        self.problem = p = problem
+        size = ctypes.c_size_t()
+        _check(load_library().ca_window_workspace_bytes(ctypes.byref(p), ctypes.byref(size)), "ca_window_workspace_bytes")
+        self.dtype = _TORCH[p.dtype]
+        self.O = torch.zeros((p.batch, p.heads_q, p.n_q, p.head_dim), dtype=self.dtype, device=dev)
+        self.lse = torch.zeros((p.batch, p.heads_q, p.n_q), dtype=torch.float32, device=dev)
+        self.ws = torch.zeros(size.value, dtype=torch.uint8, device=dev)
+
+    def window_attention_fwd(self, Q, K, V, len_q=None, len_k=None, out=None, want_lse: bool = True, stream=None):
+        """window_attention_fwd of the C library.  Returns (O, lse or None): the plan's buffers, O or `out`; rows
+        from len_q[b] on are left as they were."""
+        p, dt, dev = self.problem, self.dtype, self.device
+        out = self.O if out is None else out
+        q = _rows(Q, "Q", (p.batch, p.heads_q, p.n_q, p.head_dim), dt, dev)
+        k = _rows(K, "K", (p.batch, p.heads_kv, p.n_k, p.head_dim), dt, dev)
+        v = _rows(V, "V", (p.batch, p.heads_kv, p.n_k, p.head_dim), dt, dev)
+        o = _rows(out, "out", (p.batch, p.heads_q, p.n_q, p.head_dim), dt, dev)
+        lse = self.lse if want_lse else None
+        _call(load_library().window_attention_fwd, "window_attention_fwd", dev, stream, p, q, k, v,
+              _int32(len_q, "len_q", (p.batch,), dev), _int32(len_k, "len_k", (p.batch,), dev), o, _ptr(lse), _ptr(self.ws),
+              self.ws.numel())
+        return out, lse
+
+    def last_status(self) -> int:
+        """Status word that the last call left (ca_last_status; synchronises the device)."""
+        with torch.cuda.device(self.device):
+            return load_library().ca_last_status(_ptr(self.ws))
 
 
 # -- functional forms with the C names ------------------------------------------

@@ -556,6 +556,105 @@ int cluster_qk_basic(const ca_problem_t* p, const void* Q, const void* K, const 
   return CA_OK;
 }
 
+namespace {
+bool storage_ok(int head_dim, int dtype) {
+  return (head_dim == 64 || head_dim == 128) && (dtype == CA_DTYPE_FP32 || dtype == CA_DTYPE_BF16);
+}
+bool heads_ok(int batch, int heads_q, int heads_kv) {
+  return batch >= 1 && heads_q >= 1 && heads_kv >= 1 && heads_q % heads_kv == 0;
+}
+int check_cache(const ca_cache_t* c) {
+  if (!c) return CA_ERR_INVALID_ARG;
+  if (!heads_ok(c->batch, c->heads_q, c->heads_kv)) return CA_ERR_INVALID_ARG;
+  if (c->pages < 1 || c->pages_per_sequence < 1 || c->left < -1 || c->sinks < 0) return CA_ERR_INVALID_ARG;
+  if (!(c->softmax_scale >= 0.f) || isinf(c->softmax_scale)) return CA_ERR_INVALID_ARG;
+  if (!storage_ok(c->head_dim, c->dtype)) return CA_ERR_UNSUPPORTED;
+  if (c->page_rows < 16 || c->page_rows > 1024) return CA_ERR_UNSUPPORTED;
+  if (c->batch > 65535 || c->heads_q > 65535) return CA_ERR_UNSUPPORTED;
+  // positions of rows, and (sequence, head) pairs, are 32-bit numbers
+  if ((long long)c->pages_per_sequence * c->page_rows > 0x7fff0000LL || (long long)c->batch * c->heads_q > 0x7fffffffLL)
+    return CA_ERR_UNSUPPORTED;
+  return CA_OK;
+}
+int check_window(const ca_window_t* p) {
+  if (!p) return CA_ERR_INVALID_ARG;
+  if (!heads_ok(p->batch, p->heads_q, p->heads_kv)) return CA_ERR_INVALID_ARG;
+  if (p->n_q < 1 || p->n_k < 1 || p->left < -1 || p->right < -1 || p->sinks < 0) return CA_ERR_INVALID_ARG;
+  if (!(p->softmax_scale >= 0.f) || isinf(p->softmax_scale)) return CA_ERR_INVALID_ARG;
+  if (p->flags & ~CA_ATTN_FP32) return CA_ERR_INVALID_ARG;
+  if (!storage_ok(p->head_dim, p->dtype)) return CA_ERR_UNSUPPORTED;
+  if (p->batch > 65535 || p->heads_q > 65535 || p->n_q > 0x7fff0000 || p->n_k > 0x7fff0000) return CA_ERR_UNSUPPORTED;
+  return CA_OK;
+}
+float scale_of(float softmax_scale, int head_dim) { return softmax_scale > 0.f ? softmax_scale : 1.0f / sqrtf((float)head_dim); }
+}  // namespace
+
+int rotary_axes(const ca_rotary_t* rot, int32_t batch, int32_t heads_q, int32_t heads_k, int32_t n, int32_t head_dim,
+                int32_t dtype, int32_t inverse, const ca_rows_t* Q, const ca_rows_t* K, const int32_t* positions,
+                int64_t pos_stride_b, const ca_rows_t* Qo, const ca_rows_t* Ko, void* stream) {
+  if (!rot || !positions || batch < 1 || heads_q < 1 || heads_k < 0 || n < 1 || pos_stride_b < 0) return CA_ERR_INVALID_ARG;
+  if (!storage_ok(head_dim, dtype) || heads_q > 65535 || heads_k > 65535) return CA_ERR_UNSUPPORTED;
+  CA_TRY(check_rows(Q, batch, heads_q, n, head_dim, dtype, false));
+  CA_TRY(check_rows(Qo, batch, heads_q, n, head_dim, dtype, true));
+  if (heads_k) {
+    CA_TRY(check_rows(K, batch, heads_k, n, head_dim, dtype, false));
+    CA_TRY(check_rows(Ko, batch, heads_k, n, head_dim, dtype, true));
+  }
+  return launch_rotary_axes(*rot, batch, heads_q, heads_k, n, head_dim, dtype, inverse, Q, K, positions, pos_stride_b, Qo, Ko,
+                            static_cast<cudaStream_t>(stream));
+}
+
+int ca_cache_workspace_bytes(const ca_cache_t* c, size_t* bytes) {
+  CA_TRY(check_cache(c));
+  if (bytes) *bytes = paged_workspace_bytes(*c);
+  return CA_OK;
+}
+
+int cache_append(const ca_cache_t* c, int32_t n, const ca_rows_t* K, const ca_rows_t* V, const int32_t* lengths,
+                 const int32_t* count, const int32_t* page_table, const ca_rotary_t* rot, const int32_t* positions,
+                 int64_t pos_stride_b, void* K_pages, void* V_pages, void* ws, size_t ws_bytes, void* stream) {
+  CA_TRY(check_cache(c));
+  if (n < 1 || !lengths || !page_table || (rot && (!positions || pos_stride_b < 0))) return CA_ERR_INVALID_ARG;
+  CA_TRY(check_rows(K, c->batch, c->heads_kv, n, c->head_dim, c->dtype, false));
+  CA_TRY(check_rows(V, c->batch, c->heads_kv, n, c->head_dim, c->dtype, false));
+  if (!K_pages || !V_pages || !aligned16(K_pages) || !aligned16(V_pages)) return CA_ERR_INVALID_ARG;
+  if (!ws || !aligned16(ws) || ws_bytes < paged_workspace_bytes(*c)) return CA_ERR_WORKSPACE;
+  return launch_cache_append(*c, n, K, V, lengths, count, page_table, rot, positions, pos_stride_b, K_pages, V_pages,
+                             static_cast<int*>(ws), static_cast<cudaStream_t>(stream));
+}
+
+int paged_attention_fwd(const ca_cache_t* c, const ca_rows_t* Q, const void* K_pages, const void* V_pages,
+                        const int32_t* lengths, int32_t appended, const int32_t* page_table, const ca_rows_t* O, float* lse,
+                        void* ws, size_t ws_bytes, void* stream) {
+  CA_TRY(check_cache(c));
+  if (!lengths || !page_table || appended < 0) return CA_ERR_INVALID_ARG;
+  CA_TRY(check_rows(Q, c->batch, c->heads_q, 1, c->head_dim, c->dtype, false));
+  CA_TRY(check_rows(O, c->batch, c->heads_q, 1, c->head_dim, c->dtype, true));
+  if (!K_pages || !V_pages || !aligned16(K_pages) || !aligned16(V_pages)) return CA_ERR_INVALID_ARG;
+  if (!ws || !aligned16(ws) || ws_bytes < paged_workspace_bytes(*c)) return CA_ERR_WORKSPACE;
+  return launch_paged(*c, Q, K_pages, V_pages, lengths, appended, page_table, scale_of(c->softmax_scale, c->head_dim), O, lse, ws,
+                      static_cast<cudaStream_t>(stream));
+}
+
+int ca_window_workspace_bytes(const ca_window_t* p, size_t* bytes) {
+  CA_TRY(check_window(p));
+  if (bytes) *bytes = window_workspace_bytes(*p);
+  return CA_OK;
+}
+
+int window_attention_fwd(const ca_window_t* p, const ca_rows_t* Q, const ca_rows_t* K, const ca_rows_t* V,
+                         const int32_t* len_q, const int32_t* len_k, const ca_rows_t* O, float* lse, void* ws,
+                         size_t ws_bytes, void* stream) {
+  CA_TRY(check_window(p));
+  CA_TRY(check_rows(Q, p->batch, p->heads_q, p->n_q, p->head_dim, p->dtype, false));
+  CA_TRY(check_rows(K, p->batch, p->heads_kv, p->n_k, p->head_dim, p->dtype, false));
+  CA_TRY(check_rows(V, p->batch, p->heads_kv, p->n_k, p->head_dim, p->dtype, false));
+  CA_TRY(check_rows(O, p->batch, p->heads_q, p->n_q, p->head_dim, p->dtype, true));
+  if (!ws || !aligned16(ws) || ws_bytes < window_workspace_bytes(*p)) return CA_ERR_WORKSPACE;
+  return launch_window(*p, Q, K, V, len_q, len_k, scale_of(p->softmax_scale, p->head_dim), O, lse, ws,
+                       static_cast<cudaStream_t>(stream));
+}
+
 int ca_attn_recomputed(const void* ws) {
   if (!ws) return -CA_ERR_INVALID_ARG;
   int count = 0;

@@ -95,6 +95,25 @@ int launch_attn_ref(const ca_problem_t& pr, const void* Qp, const void* Kp, cons
                     float* lse, int* status, LaunchStream st, const int32_t* redo = nullptr, int redo_tiles = 0,
                     int* redo_count = nullptr);
 
+// rotary.cu
+int check_rows(const ca_rows_t* x, int batch, int heads, int n, int D, int dtype, bool written);
+int launch_rotary_axes(const ca_rotary_t& rot, int batch, int heads_q, int heads_k, int n, int D, int dtype, int inverse,
+                       const ca_rows_t* Q, const ca_rows_t* K, const int32_t* positions, long long pos_b, const ca_rows_t* Qo,
+                       const ca_rows_t* Ko, LaunchStream st);
+int launch_cache_append(const ca_cache_t& c, int n, const ca_rows_t* K, const ca_rows_t* V, const int32_t* lengths,
+                        const int32_t* count, const int32_t* page_table, const ca_rotary_t* rot, const int32_t* positions,
+                        long long pos_b, void* K_pages, void* V_pages, int* status, LaunchStream st);
+
+// paged.cu
+size_t paged_workspace_bytes(const ca_cache_t& c);
+int launch_paged(const ca_cache_t& c, const ca_rows_t* Q, const void* K_pages, const void* V_pages, const int32_t* lengths, int appended,
+                 const int32_t* page_table, float scale, const ca_rows_t* O, float* lse, void* ws, LaunchStream st);
+
+// window.cuh, window_ref.cu
+size_t window_workspace_bytes(const ca_window_t& p);
+int launch_window(const ca_window_t& p, const ca_rows_t* Q, const ca_rows_t* K, const ca_rows_t* V, const int32_t* len_q,
+                  const int32_t* len_k, float scale, const ca_rows_t* O, float* lse, void* ws, LaunchStream st);
+
 // attn_tc.cu
 bool attn_tc_supported(const ca_problem_t& pr);
 bool attn_tc_fp8_supported(const ca_problem_t& pr);

@@ -1,0 +1,344 @@
+// Rotary positions with several axes, on the way from the projections' layout to rows, and rows put into the
+// pages of a cache (keys rotated on the way).
+//
+// A pair of channels (x, y) of axis a turns by t = position[a] * frequency:
+//     (x, y) -> (x cos t - y sin t, x sin t + y cos t),          the inverse by -t.
+// Positions are whole numbers, so t / (2 pi) is only needed modulo 1: the host turns a frequency into a 64-bit
+// fraction of a turn, and the product with the position modulo 2^64 is the phase, to 2^-64 of a turn per step at any
+// distance, without a double in the kernel.
+//
+// What bounds it: memory.  Every element is read and written once in 16-byte vectors; a thread keeps the sines
+// and cosines of its channels and goes through heads with them, which share the positions of a row.
+#include <math.h>
+
+#include <type_traits>
+
+#include "kernels.h"
+
+namespace ca {
+
+constexpr int kMaxPairs = 64;
+
+struct RotaryTable {
+  unsigned long long turns[kMaxPairs];       // 2^64 frequency / (2 pi) modulo 2^64
+  unsigned char axis[kMaxPairs];
+  int pairs, axes;
+};
+
+// A set of heads that is read and written: [batch, heads, rows, head_dim] by strides in elements.
+struct RowSet {
+  const void* in;
+  void* out;
+  long long in_b, in_h, in_n, out_b, out_h, out_n;
+  int heads;
+  int rotate;
+};
+
+struct RotaryParams {
+  RowSet set[2];
+  const int32_t* positions;
+  long long pos_b;
+  int n, rows_per_block, items, heads_per_thread, inverse;
+  // pages (kPaged): out is a pool [pages][heads][page_rows][D]
+  const int32_t *lengths, *count, *page_table;
+  int page_rows, pages, pages_per_sequence, batch;
+  int* status;
+};
+
+// how pairs lie: none, neighbours, halves a vector at a time, halves an element at a time (where the half does not start at a vector)
+enum { kNoPairs = 0, kAdjacent = 1, kHalves = 2, kHalvesScalar = 3 };
+
+template <typename T, int W>
+struct Vec;
+template <>
+struct Vec<float, 4> { using type = uint4; };
+template <>
+struct Vec<__nv_bfloat16, 8> { using type = uint4; };
+template <>
+struct Vec<float, 1> { using type = uint32_t; };
+template <>
+struct Vec<__nv_bfloat16, 1> { using type = uint16_t; };
+
+template <typename T, int W>
+union Pack {
+  typename Vec<T, W>::type raw;
+  T e[W];
+  __device__ __forceinline__ Pack() {}
+};
+
+template <typename T>
+__device__ __forceinline__ void turn(T& x, T& y, float c, float s) {
+  const float a = to_f32<T>(x), b = to_f32<T>(y);
+  x = from_f32<T>(fmaf(a, c, -(b * s)));
+  y = from_f32<T>(fmaf(a, s, b * c));
+}
+
+// An item of a row: a vector of it, or with halves a vector of the first half and its partner.  Threads of a
+// block: rows_per_block rows by the items of a row; blockIdx.y: heads; blockIdx.z: batch.
+template <typename T, int D, int PAIRS, bool PAGED>
+__global__ void __launch_bounds__(256) rotary_kernel(const __grid_constant__ RotaryTable table,
+                                                     const __grid_constant__ RotaryParams prm) {
+  wait_for_previous();
+  constexpr int W = PAIRS == kHalvesScalar ? 1 : 16 / (int)sizeof(T);
+  constexpr bool HALVES = PAIRS == kHalves || PAIRS == kHalvesScalar;
+  constexpr int ANGLES = PAIRS == kNoPairs ? 1 : HALVES ? W : W / 2;
+  __shared__ unsigned long long s_turns[kMaxPairs];
+  __shared__ unsigned char s_axis[kMaxPairs];
+  if (PAIRS != kNoPairs) {
+    if (threadIdx.x < kMaxPairs) {
+      s_turns[threadIdx.x] = table.turns[threadIdx.x];
+      s_axis[threadIdx.x] = table.axis[threadIdx.x];
+    }
+    __syncthreads();
+  }
+  let_next_start();
+  const int b = blockIdx.z;
+  if (PAGED && blockIdx.x == 0 && blockIdx.y == 0 && b == 0) {
+    // This block looks at every index of the call and writes the status word, so that nothing has to clear it first.
+    int bad = 0;
+    const int most = prm.n / prm.page_rows + 2;
+    for (long long e = threadIdx.x; e < (long long)prm.batch * most; e += blockDim.x) {
+      const int s = (int)(e / most), part = (int)(e % most);
+      const int start = prm.lengths[s], count = prm.count ? prm.count[s] : prm.n;
+      bad |= start < 0 || count < 0 || count > prm.n;
+      const long long first = max(start, 0), last = first + min(max(count, 0), prm.n) - 1;
+      const long long page = first / prm.page_rows + part;
+      if (page > last / prm.page_rows || last < first) continue;
+      if (page >= prm.pages_per_sequence) bad = 1;
+      else bad |= (unsigned)prm.page_table[(size_t)s * prm.pages_per_sequence + page] >= (unsigned)prm.pages;
+    }
+    bad = __syncthreads_or(bad);
+    if (threadIdx.x == 0) *prm.status = bad ? CA_ERR_BAD_INDEX : CA_OK;
+  }
+  const int item = threadIdx.x % prm.items, sub = threadIdx.x / prm.items;
+  const long long row = (long long)blockIdx.x * prm.rows_per_block + sub;
+  if (sub >= prm.rows_per_block || row >= prm.n) return;
+
+  long long slot = 0;                                    // first element of the row's place in a pool, of head 0
+  if (PAGED) {
+    const int start = prm.lengths[b], count = prm.count ? prm.count[b] : prm.n;
+    if (start < 0 || row >= count) return;               // (a row that is not there)
+    const long long at = start + row, page = at / prm.page_rows;
+    if (page >= prm.pages_per_sequence) return;
+    const int id = prm.page_table[(size_t)b * prm.pages_per_sequence + page];
+    if ((unsigned)id >= (unsigned)prm.pages) return;
+    slot = ((long long)id * prm.set[0].heads * prm.page_rows + at % prm.page_rows) * D;
+  }
+
+  // ---- sines and cosines of this thread's pairs; a pair behind the last one stays as it is
+  const int R = PAIRS == kNoPairs ? 0 : table.pairs;
+  const int lead = HALVES ? R / W : 0;                   // items with a partner
+  const bool both = HALVES && item < lead;
+  const int first = !HALVES ? item * W : both ? item * W : 2 * R + (item - lead) * W;
+  const int partner = first + R;
+  float cs[ANGLES], sn[ANGLES];
+  int turned = 0;
+  if (PAIRS != kNoPairs) {
+    const int32_t* pos = prm.positions + b * prm.pos_b + row * table.axes;
+    const int pair0 = HALVES ? item * W : item * (W / 2);
+#pragma unroll
+    for (int i = 0; i < ANGLES; ++i) {
+      const int pair = pair0 + i;
+      cs[i] = 1.f;
+      sn[i] = 0.f;
+      if (pair < R) {
+        const unsigned long long phase = (unsigned long long)(long long)pos[s_axis[pair]] * s_turns[pair];
+        sincospif((float)(long long)phase * 0x1p-63f, &sn[i], &cs[i]);
+        if (prm.inverse) sn[i] = -sn[i];
+        turned = i + 1;
+      }
+    }
+  }
+
+  auto go = [&](const RowSet& set, int h0, int h1, bool rotate) {
+    using P = Pack<T, W>;
+    const T* in = static_cast<const T*>(set.in) + b * set.in_b + row * set.in_n + first;
+    T* out = static_cast<T*>(set.out) + (PAGED ? slot : b * set.out_b + row * set.out_n) + first;
+    const long long out_h = PAGED ? (long long)prm.page_rows * D : set.out_h;
+    auto some = [&](int h, auto count) {
+      constexpr int N = decltype(count)::value;
+      P x[N], y[N];
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        x[j].raw = *reinterpret_cast<const typename Vec<T, W>::type*>(in + (h + j) * set.in_h);
+        if (both) y[j].raw = *reinterpret_cast<const typename Vec<T, W>::type*>(in + (h + j) * set.in_h + (partner - first));
+      }
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        if (PAIRS != kNoPairs && rotate) {
+          if (HALVES) {
+            if (both) {
+#pragma unroll
+              for (int i = 0; i < ANGLES; ++i) turn(x[j].e[i], y[j].e[i], cs[i], sn[i]);
+            }
+          } else {
+#pragma unroll
+            for (int i = 0; i < ANGLES; ++i)
+              if (i < turned) turn(x[j].e[2 * i % W], x[j].e[(2 * i + 1) % W], cs[i], sn[i]);
+          }
+        }
+        *reinterpret_cast<typename Vec<T, W>::type*>(out + (h + j) * out_h) = x[j].raw;
+        if (both) *reinterpret_cast<typename Vec<T, W>::type*>(out + (h + j) * out_h + (partner - first)) = y[j].raw;
+      }
+    };
+    int h = h0;
+    for (; h + 4 <= h1; h += 4) some(h, std::integral_constant<int, 4>{});
+    for (; h < h1; ++h) some(h, std::integral_constant<int, 1>{});
+  };
+  const int begin = blockIdx.y * prm.heads_per_thread;
+  const int end = min(begin + prm.heads_per_thread, prm.set[0].heads + prm.set[1].heads);
+  const int mid = min(max(prm.set[0].heads, begin), end);
+  if (begin < mid) go(prm.set[0], begin, mid, prm.set[0].rotate != 0);
+  if (mid < end) go(prm.set[1], mid - prm.set[0].heads, end - prm.set[0].heads, prm.set[1].rotate != 0);
+}
+
+// ---- host side -------------------------------------------------------------------------------------------
+
+// frequency / (2 pi) modulo 1 as a 64-bit fraction, rounded: the frequency's 53-bit mantissa times 128 bits of 1 / (2 pi), so that the
+// fraction is right to its last bit up to 2^32 radians per step.
+static unsigned long long turn_fraction(double freq) {
+  constexpr unsigned long long kHi = 0x28BE60DB9391054Aull, kLo = 0x7F09D5F47D4D3770ull;   // 2^128 / (2 pi)
+  int exponent = 0;
+  const double m = frexp(fabs(freq), &exponent);
+  const unsigned long long M = (unsigned long long)ldexp(m, 53);
+  const unsigned __int128 low = (unsigned __int128)M * kLo, high = (unsigned __int128)M * kHi + (low >> 64);
+  // the product is (high, low's lower word) 2^(exponent - 53 - 128) turns; word `shift` bits up is the fraction
+  const unsigned long long w[4] = {(unsigned long long)low, (unsigned long long)high, (unsigned long long)(high >> 64), 0ull};
+  const int shift = 64 - (exponent - 53);
+  unsigned long long r = 0;
+  if (shift < 193) {
+    const int word = (shift - 1) / 64, bit = (shift - 1) % 64;         // one bit more, to round
+    auto at = [&](int i) { return i < 3 ? w[i] : 0ull; };
+    const unsigned __int128 two = ((unsigned __int128)at(word + 1) << 64) | at(word);
+    const unsigned long long below = (unsigned long long)(two >> bit);
+    const unsigned long long top = (unsigned long long)(((((unsigned __int128)at(word + 2) << 64) | at(word + 1)) >> bit) & 1u);
+    r = (below >> 1) + (top << 63) + (below & 1u);
+  }
+  return freq < 0 ? 0ull - r : r;
+}
+
+static int make_table(const ca_rotary_t& rot, int D, RotaryTable* table) {
+  if (rot.axes < 1 || rot.axes > 4 || !rot.freq) return CA_ERR_INVALID_ARG;
+  table->axes = rot.axes;
+  int n = 0;
+  for (int a = 0; a < rot.axes; ++a) {
+    if (rot.pairs[a] < 0 || rot.pairs[a] > D / 2 - n) return CA_ERR_INVALID_ARG;
+    for (int i = 0; i < rot.pairs[a]; ++i, ++n) {
+      if (!(fabs(rot.freq[n]) <= 4294967296.0)) return CA_ERR_INVALID_ARG;
+      table->turns[n] = turn_fraction(rot.freq[n]);
+      table->axis[n] = (unsigned char)a;
+    }
+  }
+  if (n < 1) return CA_ERR_INVALID_ARG;
+  table->pairs = n;
+  return CA_OK;
+}
+
+template <typename T, int D, bool PAGED>
+static int launch_rotary_d(const RotaryTable& table, RotaryParams& prm, int pairs_mode, int batch, LaunchStream st) {
+  constexpr int W = 16 / (int)sizeof(T);
+  const int R = table.pairs;
+  if (pairs_mode == kHalves && R % W != 0) pairs_mode = kHalvesScalar;
+  const int w = pairs_mode == kHalvesScalar ? 1 : W;
+  prm.items = pairs_mode == kHalves || pairs_mode == kHalvesScalar ? D / w - R / w : D / W;
+  prm.rows_per_block = 256 / prm.items;
+  const int heads = prm.set[0].heads + prm.set[1].heads;
+  const long long blocks_n = ((long long)prm.n + prm.rows_per_block - 1) / prm.rows_per_block;
+  // heads per thread: its sines and cosines serve 8, fewer where that leaves SMs without blocks
+  int per = 8;
+  while (per > 1 && blocks_n * batch * ((heads + per - 1) / per) < 2 * 148) per /= 2;
+  prm.heads_per_thread = per;
+  const dim3 grid((unsigned)blocks_n, (unsigned)((heads + per - 1) / per), (unsigned)batch);
+  if (blocks_n > 0x7fffffffLL || grid.y > 65535u || batch > 65535) return CA_ERR_UNSUPPORTED;
+  auto go = [&](auto mode) -> int {
+    launch_chained(rotary_kernel<T, D, decltype(mode)::value, PAGED>, grid, 256, 0, st, table, prm);
+    CA_LAUNCH_CHECK();
+    return CA_OK;
+  };
+  switch (pairs_mode) {
+    case kNoPairs: return go(std::integral_constant<int, kNoPairs>{});
+    case kAdjacent: return go(std::integral_constant<int, kAdjacent>{});
+    case kHalves: return go(std::integral_constant<int, kHalves>{});
+    default: return go(std::integral_constant<int, kHalvesScalar>{});
+  }
+}
+
+template <bool PAGED>
+static int launch_rotary(const RotaryTable& table, RotaryParams& prm, int mode, int batch, int D, int dtype, LaunchStream st) {
+  if (dtype == CA_DTYPE_BF16)
+    return D == 64 ? launch_rotary_d<__nv_bfloat16, 64, PAGED>(table, prm, mode, batch, st)
+                   : launch_rotary_d<__nv_bfloat16, 128, PAGED>(table, prm, mode, batch, st);
+  return D == 64 ? launch_rotary_d<float, 64, PAGED>(table, prm, mode, batch, st)
+                 : launch_rotary_d<float, 128, PAGED>(table, prm, mode, batch, st);
+}
+
+int check_rows(const ca_rows_t* x, int batch, int heads, int n, int D, int dtype, bool written) {
+  if (!x || !x->data || (reinterpret_cast<uintptr_t>(x->data) & 15u)) return CA_ERR_INVALID_ARG;
+  const long long vec = dtype == CA_DTYPE_BF16 ? 8 : 4;
+  const long long stride[3] = {x->stride_b, x->stride_h, x->stride_n};
+  const int extent[3] = {batch, heads, n};
+  for (int i = 0; i < 3; ++i) {
+    if (extent[i] <= 1) continue;                          // a stride that nothing is multiplied with
+    if (stride[i] % vec != 0) return CA_ERR_INVALID_ARG;
+    if (written && stride[i] < D) return CA_ERR_INVALID_ARG;   // rows of an output do not overlap
+  }
+  return CA_OK;
+}
+
+static RowSet row_set(const ca_rows_t* in, const ca_rows_t* out, int heads, int rotate) {
+  RowSet s{};
+  s.in = in->data;
+  s.in_b = in->stride_b; s.in_h = in->stride_h; s.in_n = in->stride_n;
+  if (out) {
+    s.out = out->data;
+    s.out_b = out->stride_b; s.out_h = out->stride_h; s.out_n = out->stride_n;
+  }
+  s.heads = heads;
+  s.rotate = rotate;
+  return s;
+}
+
+int launch_rotary_axes(const ca_rotary_t& rot, int batch, int heads_q, int heads_k, int n, int D, int dtype, int inverse,
+                       const ca_rows_t* Q, const ca_rows_t* K, const int32_t* positions, long long pos_b, const ca_rows_t* Qo,
+                       const ca_rows_t* Ko, LaunchStream st) {
+  RotaryTable table{};
+  const int rc = make_table(rot, D, &table);
+  if (rc != CA_OK) return rc;
+  RotaryParams prm{};
+  if (heads_q) prm.set[0] = row_set(Q, Qo, heads_q, 1);
+  if (heads_k) prm.set[1] = row_set(K, Ko, heads_k, 1);
+  prm.positions = positions;
+  prm.pos_b = pos_b;
+  prm.n = n;
+  prm.inverse = inverse;
+  return launch_rotary<false>(table, prm, rot.adjacent ? kAdjacent : kHalves, batch, D, dtype, st);
+}
+
+int launch_cache_append(const ca_cache_t& c, int n, const ca_rows_t* K, const ca_rows_t* V, const int32_t* lengths,
+                        const int32_t* count, const int32_t* page_table, const ca_rotary_t* rot, const int32_t* positions,
+                        long long pos_b, void* K_pages, void* V_pages, int* status, LaunchStream st) {
+  RotaryTable table{};
+  if (rot) {
+    const int rc = make_table(*rot, c.head_dim, &table);
+    if (rc != CA_OK) return rc;
+  }
+  RotaryParams prm{};
+  prm.set[0] = row_set(K, nullptr, c.heads_kv, 1);
+  prm.set[1] = row_set(V, nullptr, c.heads_kv, 0);
+  prm.set[0].out = K_pages;
+  prm.set[1].out = V_pages;
+  prm.positions = positions;
+  prm.pos_b = pos_b;
+  prm.n = n;
+  prm.lengths = lengths;
+  prm.count = count;
+  prm.page_table = page_table;
+  prm.page_rows = c.page_rows;
+  prm.pages = c.pages;
+  prm.pages_per_sequence = c.pages_per_sequence;
+  prm.batch = c.batch;
+  prm.status = status;
+  return launch_rotary<true>(table, prm, !rot ? kNoPairs : rot->adjacent ? kAdjacent : kHalves, c.batch, c.head_dim, c.dtype, st);
+}
+
+}  // namespace ca

@@ -1,0 +1,253 @@
+"""Attention over a sliding window with first tokens that stay visible, against the plain form in 64 bits."""
+import math
+
+import pytest
+import torch
+
+import streams_reference as ref
+from paper_2608_26965_b200 import binding
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+DT = {"fp32": torch.float32, "bf16": torch.bfloat16}
+KERNELS = [("bf16", 0), ("bf16", binding.CA_ATTN_FP32), ("fp32", 0)]
+
+
+def generator(seed):
+    g = torch.Generator(device=DEV)
+    g.manual_seed(seed)
+    return g
+
+
+def rows(g, shape, dtype, layout="dense", gain=1.0):
+    B, H, n, d = shape
+    if layout == "rows_first":
+        return (torch.randn((B, n, H, d), generator=g, device=DEV) * gain).to(DT[dtype]).transpose(1, 2)
+    if layout == "room":
+        return (torch.randn((B, H, n, d + 16), generator=g, device=DEV) * gain).to(DT[dtype])[..., 8:8 + d]
+    return (torch.randn(shape, generator=g, device=DEV) * gain).to(DT[dtype])
+
+
+def check(p, q, k, v, O, lse, len_q=None, len_k=None, heads=None, weights16=None):
+    scale = p.softmax_scale if p.softmax_scale > 0 else 1 / math.sqrt(p.head_dim)
+    group = p.heads_q // p.heads_kv
+    dt = O.dtype
+    weights16 = dt == torch.bfloat16 and not p.flags if weights16 is None else weights16
+    for b in range(p.batch):
+        a, n = (p.n_q if len_q is None else len_q[b]), (p.n_k if len_k is None else len_k[b])
+        see = ref.window_mask(a, n, p.left, p.right, p.sinks, DEV)
+        for h in heads or range(p.heads_q):
+            want, l64, bound, lb, empty = ref.attend(q[b, h, :a].double(), k[b, h // group, :n].double(), v[b, h // group, :n].double(), see, scale,
+                                                     dt, weights16)
+            ref.check(O[b, h, :a], want, bound, f"item {b}, head {h}")
+            ref.check_lse(lse[b, h, :a].double(), l64, lb, empty, f"item {b}, head {h}")
+
+
+def run(p, q, k, v, **kw):
+    plan = binding.WindowPlan(p, DEV)
+    O, lse = plan.window_attention_fwd(q, k, v, **kw)
+    assert plan.last_status() == 0
+    return O, lse
+
+
+@pytest.mark.parametrize("dtype,flags", KERNELS)
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("n_q,n_k", [(1, 1), (1, 200), (7, 5), (64, 64), (127, 127), (128, 128), (129, 129), (200, 131), (131, 300), (257, 513),
+                                     (600, 600)])
+@pytest.mark.parametrize("left,right,sinks", [(-1, -1, 0), (-1, 0, 0), (0, 0, 0), (10, 0, 4), (100, 30, 1), (5, -1, 140), (64, 63, 0), (130, 0, 260)])
+def test_sizes_and_windows(dtype, flags, d, n_q, n_k, left, right, sinks):
+    g = generator(n_q + n_k + left)
+    p = binding.make_window_problem(2, 2, 1, n_q, n_k, d, dtype, left, right, sinks, flags=flags)
+    q, k, v = rows(g, (2, 2, n_q, d), dtype, gain=1.5), rows(g, (2, 1, n_k, d), dtype), rows(g, (2, 1, n_k, d), dtype)
+    check(p, q, k, v, *run(p, q, k, v))
+
+
+@pytest.mark.parametrize("dtype,flags", KERNELS)
+@pytest.mark.parametrize("hq,kv", [(1, 1), (6, 3), (5, 1), (16, 2)])
+@pytest.mark.parametrize("layout", ["rows_first", "room"])
+def test_heads_and_strides(dtype, flags, hq, kv, layout):
+    g = generator(hq)
+    n, d = 333, 64
+    p = binding.make_window_problem(2, hq, kv, n, n, d, dtype, 50, 20, 3, softmax_scale=0.3, flags=flags)
+    q, k, v = rows(g, (2, hq, n, d), dtype, layout), rows(g, (2, kv, n, d), dtype, layout), rows(g, (2, kv, n, d), dtype, "dense")
+    room = torch.full((2, n, hq, d + 8), 9.0, dtype=DT[dtype], device=DEV)
+    O, lse = run(p, q, k, v, out=room.transpose(1, 2)[..., :d])
+    check(p, q, k, v, O, lse)
+    assert (room[..., d:] == 9.0).all()
+
+
+@pytest.mark.parametrize("dtype,flags", KERNELS)
+@pytest.mark.parametrize("d,left,right,sinks", [(64, 40, 0, 4), (128, -1, 0, 0), (128, 20, 7, 130)])
+def test_ragged_batch(dtype, flags, d, left, right, sinks):
+    """What stands behind a sequence is not a number and is not used; rows behind it are left as they were; more queries than
+    keys leave rows that see nothing."""
+    g = generator(d)
+    len_q, len_k = [300, 1, 0, 129, 64, 300, 200], [300, 300, 77, 0, 10, 128, 200]
+    B, n = len(len_q), 300
+    p = binding.make_window_problem(B, 2, 2, n, n, d, dtype, left, right, sinks, flags=flags)
+    q, k, v = (rows(g, (B, 2, n, d), dtype, "rows_first") for _ in range(3))
+    for b in range(B):
+        q[b, :, len_q[b]:] = float("nan")
+        k[b, :, len_k[b]:] = float("nan")
+        v[b, :, len_k[b]:] = float("inf")
+    plan = binding.WindowPlan(p, DEV)
+    plan.O.fill_(5.0)
+    plan.lse.fill_(6.0)
+    lq, lk = (torch.tensor(x, dtype=torch.int32, device=DEV) for x in (len_q, len_k))
+    O, lse = plan.window_attention_fwd(q, k, v, len_q=lq, len_k=lk)
+    assert plan.last_status() == 0
+    check(p, q, k, v, O, lse, len_q, len_k)
+    for b in range(B):
+        assert (O[b, :, len_q[b]:] == 5.0).all() and (lse[b, :, len_q[b]:] == 6.0).all()
+    # only one of the two
+    O, lse = run(p, torch.nan_to_num(q), k, v, len_k=lk)
+    check(p, torch.nan_to_num(q), k, v, O, lse, None, len_k)
+    # lengths that are none: cut, recorded
+    lq[0], lk[1] = 301, -1
+    plan.window_attention_fwd(q, k, v, len_q=lq, len_k=lk)
+    assert plan.last_status() == binding.CA_ERR_BAD_INDEX
+    lq[0], lk[1] = 300, 300
+    plan.window_attention_fwd(q, k, v, len_q=lq, len_k=lk)
+    assert plan.last_status() == 0
+
+
+@pytest.mark.parametrize("dtype,flags", KERNELS)
+@pytest.mark.parametrize("left,right,sinks", [(300, 0, 20), (700, 700, 0), (-1, 0, 0), (1, 1, 1000)])
+def test_long(dtype, flags, left, right, sinks):
+    g = generator(17)
+    n, d = 2500, 128
+    p = binding.make_window_problem(1, 3, 1, n, n, d, dtype, left, right, sinks, flags=flags)
+    q, k, v = rows(g, (1, 3, n, d), dtype, "rows_first", 2.0), rows(g, (1, 1, n, d), dtype, "rows_first"), rows(g, (1, 1, n, d), dtype)
+    O, lse = run(p, q, k, v)
+    check(p, q, k, v, O, lse)
+    again = run(p, q, k, v)
+    assert torch.equal(O, again[0]) and torch.equal(lse, again[1])
+
+
+@pytest.mark.parametrize("dtype,flags", KERNELS)
+def test_scores_that_climb_and_fall(dtype, flags):
+    """The reference of the softmax moves from tile to tile, by more than 2^96 too."""
+    n, d = 1000, 64
+    g = generator(2)
+    p = binding.make_window_problem(1, 2, 2, n, n, d, dtype, -1, -1, 0, softmax_scale=1.0, flags=flags)
+    q, k, v = (rows(g, (1, 2, n, d), dtype, gain=0.1) for _ in range(3))
+    q[..., 0] = 1.0
+    ramp = torch.linspace(-300, 300, n, device=DEV).to(DT[dtype])
+    k[0, 0, :, 0], k[0, 1, :, 0] = ramp, ramp.flip(0)
+    check(p, q, k, v, *run(p, q, k, v))
+
+
+@pytest.mark.parametrize("dtype,flags", KERNELS)
+@pytest.mark.parametrize("d", [64, 128])
+def test_values_that_are_not_numbers_outside_the_window(dtype, flags, d):
+    """What a row does not see takes no part in it, in the same tile of keys too; rows that see it are not numbers."""
+    n = 400
+    g = generator(d)
+    p = binding.make_window_problem(1, 1, 1, n, n, d, dtype, 30, 5, 2, flags=flags)
+    q, k, v = (rows(g, (1, 1, n, d), dtype) for _ in range(3))
+    clean = run(p, q, k, v)
+    v2, k2 = v.clone(), k.clone()
+    v2[0, 0, 150] = float("nan")
+    v2[0, 0, 290, 3] = float("inf")
+    k2[0, 0, 220] = float("nan")
+    O, lse = run(p, q, k2, v2)
+    i = torch.arange(n, device=DEV)
+    sees = lambda j: (j <= i + 5) & (j >= i - 30)
+    assert torch.isnan(O[0, 0, sees(150)].float()).all() and torch.isnan(O[0, 0, sees(220)].float()).all()
+    assert torch.isinf(O[0, 0, sees(290), 3].float()).all()
+    rest = ~(sees(150) | sees(290) | sees(220))
+    see = ref.window_mask(n, n, 30, 5, 2, DEV)
+    see[~rest] = False
+    want, l64, bound, lb, empty = ref.attend(q[0, 0].double(), k[0, 0].double(), v[0, 0].double(), see, 1 / math.sqrt(d), DT[dtype],
+                                             dtype == "bf16" and not flags)
+    ref.check(O[0, 0, rest], want[rest], bound[rest], "rows that do not see them")
+    # a value that is not a number leaves the weights as they are
+    assert torch.equal(lse[0, 0, ~sees(220)], clean[1][0, 0, ~sees(220)])
+    assert torch.isnan(lse[0, 0, sees(220)]).all()
+
+
+def test_large_values_next_to_masked_ones():
+    """Values near the end of the type's range, and keys whose scores are the lowest and the highest."""
+    n, d = 300, 64
+    g = generator(8)
+    for dtype, flags in KERNELS:
+        p = binding.make_window_problem(1, 1, 1, n, n, d, dtype, 20, 0, 1, flags=flags)
+        q, k, v = (rows(g, (1, 1, n, d), dtype) for _ in range(3))
+        v[0, 0, 100:110] *= 1e37
+        k[0, 0, 200] = 1e4 * q[0, 0, 210]
+        k[0, 0, 201] = -1e4 * q[0, 0, 210]
+        check(p, q, k, v, *run(p, q, k, v))
+
+
+def test_graphs_streams_and_shared_workspace():
+    g = generator(4)
+    plans = []
+    for n, left in ((500, 60), (900, 200)):
+        p = binding.make_window_problem(1, 4, 2, n, n, 64, "bf16", left, 0, 4)
+        q, k, v = rows(g, (1, 4, n, 64), "bf16"), rows(g, (1, 2, n, 64), "bf16"), rows(g, (1, 2, n, 64), "bf16")
+        plan = binding.WindowPlan(p, DEV)
+        want = plan.window_attention_fwd(q, k, v)[0].clone()
+        plans.append((plan, q, k, v, want))
+    size = max(x[0].ws.numel() for x in plans)
+    shared = torch.zeros(size, dtype=torch.uint8, device=DEV)
+    kept = [x[0].ws for x in plans]
+    graphs = []
+    for plan, q, k, v, _ in plans:
+        plan.ws = shared
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            plan.window_attention_fwd(q, k, v)
+        graphs.append(graph)
+        plan.O.zero_()
+    for _ in range(2):
+        for graph in graphs:
+            graph.replay()
+    torch.cuda.synchronize()
+    for plan, q, k, v, want in plans:
+        assert torch.equal(plan.O, want)
+        plan.O.zero_()
+    streams = torch.cuda.Stream(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for x, ws, s in zip(plans, kept, streams):
+        x[0].ws = ws
+    for _ in range(10):
+        for (plan, q, k, v, _), s in zip(plans, streams):
+            plan.window_attention_fwd(q, k, v, stream=s)
+    torch.cuda.synchronize()
+    for plan, q, k, v, want in plans:
+        assert torch.equal(plan.O, want)
+
+
+@pytest.mark.parametrize("dtype,flags", KERNELS)
+def test_strides_beyond_32_bits(dtype, flags):
+    """Batch items more than 2^31 elements apart, in inputs and output."""
+    n, d = 200, 64
+    far = 2 ** 31 + 64
+    g = generator(6)
+    p = binding.make_window_problem(2, 1, 1, n, n, d, dtype, 30, 0, 2, flags=flags)
+    store = torch.empty((far + 4 * n * d,), dtype=DT[dtype], device=DEV)
+    view = lambda i: store.as_strided((2, 1, n, d), (far, n * d, d, 1), i * n * d)
+    q, k, v, out = (view(i) for i in range(4))
+    for x in (q, k, v):
+        x.copy_(rows(g, (2, 1, n, d), dtype))
+    O, lse = run(p, q, k, v, out=out)
+    check(p, q, k, v, O, lse)
+
+
+def test_same_results_as_one_token_at_a_time():
+    """The last row of a causal window and the cache's attention of one token see the same keys."""
+    g = generator(12)
+    n, d, hq, kv = 700, 128, 8, 2
+    q, k, v = rows(g, (1, hq, n, d), "bf16"), rows(g, (1, kv, n, d), "bf16"), rows(g, (1, kv, n, d), "bf16")
+    p = binding.make_window_problem(1, hq, kv, n, n, d, "bf16", 100, 0, 6)
+    O, lse = run(p, q, k, v)
+    cache = binding.PagedCache(binding.make_cache_problem(1, hq, kv, d, "bf16", 32, 22, 22, left=100, sinks=6), DEV,
+                               page_table=torch.arange(22, device=DEV).flip(0).reshape(1, 22).int().contiguous())
+    cache.cache_append(k, v)
+    cache.lengths.fill_(n)
+    one, l1 = cache.paged_attention_fwd(q[:, :, -1:])
+    see = ref.window_mask(n, n, 100, 0, 6, DEV)[-1:]
+    for h in range(hq):
+        _, _, bound, lb, _ = ref.attend(q[0, h, -1:].double(), k[0, h // 4].double(), v[0, h // 4].double(), see, 1 / math.sqrt(d), torch.bfloat16, True)
+        ref.check(one[0, h], O[0, h, -1:].double(), 2 * bound, "one token")
+        ref.check(l1[0, h], lse[0, h, -1:].double(), 2 * lb, "one token's log-sum-exp")
