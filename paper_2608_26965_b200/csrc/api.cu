@@ -584,6 +584,7 @@ int check_window(const ca_window_t* p) {
   if (p->flags & ~CA_ATTN_FP32) return CA_ERR_INVALID_ARG;
   if (!storage_ok(p->head_dim, p->dtype)) return CA_ERR_UNSUPPORTED;
   if (p->batch > 65535 || p->heads_q > 65535 || p->n_q > 0x7fff0000 || p->n_k > 0x7fff0000) return CA_ERR_UNSUPPORTED;
+  if ((long long)p->batch * p->heads_q > 0x7fffffffLL) return CA_ERR_UNSUPPORTED;
   return CA_OK;
 }
 float scale_of(float softmax_scale, int head_dim) { return softmax_scale > 0.f ? softmax_scale : 1.0f / sqrtf((float)head_dim); }

@@ -11,12 +11,14 @@ struct WindowParams {
   float* lse;                       // [batch][heads_q][n_q] or null
   const int32_t *len_q, *len_k;     // [batch] or null
   int* status;
-  int32_t* redo;                    // [batch * heads_q][tiles of kWindowTile rows]: recompute these (null: all)
+  int32_t* redo;                    // [batch * heads_q][blocks of kWindowBlock rows][8]: rows 32 at a time to compute again (null: all)
+  int32_t* redo_any;                // whether there are any
   int batch, heads_q, heads_kv, group, n_q, n_k, left, right, sinks;
   float scale_log2;
 };
 
 constexpr int kWindowTile = 128;    // query rows of a tensor-core tile
+constexpr int kWindowBlock = 256;   // two of them: what a CTA works on at a time
 
 // Lengths of a batch item, kept in range (what is out of it is flagged by check_lengths).
 struct WindowItem {
@@ -26,6 +28,7 @@ struct WindowItem {
     len_k = prm.len_k ? min(max(prm.len_k[b], 0), prm.n_k) : prm.n_k;
     shift = len_k - len_q;
   }
+  __device__ __forceinline__ WindowItem(int q, int k) : len_q(q), len_k(k), shift(k - q) {}
 };
 
 // Key tiles of U keys that rows [r0, r1) see: first tokens, then the window.
@@ -63,6 +66,6 @@ struct WindowRow {
 };
 
 int launch_window_ref(const WindowParams& prm, int D, int dtype, LaunchStream st);
-int launch_window_tc(const WindowParams& prm, int D, int* next_tile, LaunchStream st);
+int launch_window_tc(const WindowParams& prm, int D, int* next, LaunchStream st);    // CA_ERR_UNSUPPORTED: strides that it does not take
 
 }  // namespace ca

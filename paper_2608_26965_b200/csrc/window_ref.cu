@@ -26,7 +26,7 @@ __device__ __forceinline__ void window_rows_to_smem(float* dst, const T* src, lo
 }
 
 template <typename T, int D>
-__global__ void __launch_bounds__(kWrThreads) window_ref_kernel(const __grid_constant__ WindowParams prm, bool check) {
+__global__ void __launch_bounds__(kWrThreads) window_ref_kernel(const __grid_constant__ WindowParams prm) {
   wait_for_previous();
   let_next_start();
   extern __shared__ __align__(16) float smf[];
@@ -35,23 +35,34 @@ __global__ void __launch_bounds__(kWrThreads) window_ref_kernel(const __grid_con
   float* sv = sk + kWrKeys * (D + 4);
   float* sp = sv + kWrKeys * (D + 4);           // [64][68]
   const int tid = threadIdx.x, ty = tid >> 4, tx = tid & 15;
-  const int b = blockIdx.z, h = blockIdx.y, r0 = blockIdx.x * kWrRows;
-  if (check && blockIdx.x == 0 && h == 0 && b == 0) {
+  if (blockIdx.x == 0) {
     int bad = 0;
     for (int i = tid; i < prm.batch; i += kWrThreads)
       bad |= (prm.len_q && (unsigned)prm.len_q[i] > (unsigned)prm.n_q) || (prm.len_k && (unsigned)prm.len_k[i] > (unsigned)prm.n_k);
     bad = __syncthreads_or(bad);
-    if (tid == 0) *prm.status = bad ? CA_ERR_BAD_INDEX : CA_OK;
+    // the only one that writes the status word, unless the tensor-core kernel has recorded something
+    if (tid == 0 && !prm.redo) *prm.status = bad ? CA_ERR_BAD_INDEX : CA_OK;
+    if (tid == 0 && prm.redo && bad) atomicCAS(prm.status, 0, CA_ERR_BAD_INDEX);
   }
-  if (prm.redo && !prm.redo[((size_t)b * prm.heads_q + h) * ((prm.n_q + kWindowTile - 1) / kWindowTile) + r0 / kWindowTile]) return;
+  if (prm.redo && *prm.redo_any == 0) return;
+  const int blocks64 = (prm.n_q + kWrRows - 1) / kWrRows;
+  const long long n_work = (long long)blocks64 * prm.heads_q * prm.batch;
+#pragma unroll 1
+  for (long long idx = blockIdx.x; idx < n_work; idx += gridDim.x) {
+  const int r0 = (int)(idx % blocks64) * kWrRows, bh = (int)(idx / blocks64), b = bh / prm.heads_q, h = bh % prm.heads_q;
   const WindowItem it(prm, b);
-  if (r0 >= it.len_q) return;
+  if (r0 >= it.len_q) continue;
+  if (prm.redo) {
+    const int32_t* marks = prm.redo + ((size_t)bh * ((prm.n_q + kWindowBlock - 1) / kWindowBlock) + r0 / kWindowBlock) * 8 + r0 % kWindowBlock / 32;
+    if (marks[0] == 0 && marks[1] == 0) continue;
+  }
   const int rows = min(kWrRows, it.len_q - r0);
   const WindowSpan span(prm, it, r0, r0 + rows, kWrKeys);
   const int g = h / prm.group;
   const T* q = static_cast<const T*>(prm.q) + b * prm.q_b + h * prm.q_h + r0 * prm.q_n;
   const T* k = static_cast<const T*>(prm.k) + b * prm.k_b + g * prm.k_h;
   const T* v = static_cast<const T*>(prm.v) + b * prm.v_b + g * prm.v_h;
+  __syncthreads();                              // (the rows before have been worked off)
   window_rows_to_smem<T, D>(sq, q, prm.q_n, rows, tid);
 
   float o[4][D / 64][4], m[4], l[4];
@@ -156,6 +167,7 @@ __global__ void __launch_bounds__(kWrThreads) window_ref_kernel(const __grid_con
     if (tx == 0 && prm.lse)
       prm.lse[((size_t)b * prm.heads_q + h) * prm.n_q + row] = l[i] == 0.f ? -INFINITY : (m[i] + log2f(l[i])) * 0.6931471805599453f;
   }
+  }
 }
 
 template <typename T, int D>
@@ -163,7 +175,10 @@ static int launch_window_ref_d(const WindowParams& prm, LaunchStream st) {
   constexpr int smem = (3 * 64 * (D + 4) + 64 * (kWrKeys + 4)) * 4;
   auto kernel = window_ref_kernel<T, D>;
   CA_RETURN_IF_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
-  launch_chained(kernel, dim3(ceil_div(prm.n_q, kWrRows), prm.heads_q, prm.batch), kWrThreads, smem, st, prm, prm.redo == nullptr);
+  const long long n_work = (long long)ceil_div(prm.n_q, kWrRows) * prm.heads_q * prm.batch;
+  // a CTA for every 64 rows; to compute rows again, hardly ever any, as many as are on the GPU at a time
+  const long long most = prm.redo ? 296 : 0x7fffffffLL;
+  launch_chained(kernel, (unsigned)(n_work < most ? n_work : most), kWrThreads, smem, st, prm);
   CA_LAUNCH_CHECK();
   return CA_OK;
 }
@@ -175,8 +190,8 @@ int launch_window_ref(const WindowParams& prm, int D, int dtype, LaunchStream st
 }
 
 size_t window_workspace_bytes(const ca_window_t& p) {
-  (void)p;
-  return kStatusBytes;
+  // status block, marks of the rows to compute again
+  return kStatusBytes + align_up((size_t)p.batch * p.heads_q * ceil_div(p.n_q, kWindowBlock) * 8 * sizeof(int32_t), 256);
 }
 
 int launch_window(const ca_window_t& p, const ca_rows_t* Q, const ca_rows_t* K, const ca_rows_t* V, const int32_t* len_q,
@@ -192,6 +207,15 @@ int launch_window(const ca_window_t& p, const ca_rows_t* Q, const ca_rows_t* K, 
   prm.batch = p.batch; prm.heads_q = p.heads_q; prm.heads_kv = p.heads_kv; prm.group = p.heads_q / p.heads_kv;
   prm.n_q = p.n_q; prm.n_k = p.n_k; prm.left = p.left; prm.right = p.right; prm.sinks = p.sinks;
   prm.scale_log2 = scale * 1.4426950408889634f;
+  if (p.dtype == CA_DTYPE_BF16 && !(p.flags & CA_ATTN_FP32)) {
+    int* status = static_cast<int*>(ws);
+    prm.redo = status + kStatusBytes / sizeof(int);
+    prm.redo_any = status + kTileWord + 1;
+    const int rc = launch_window_tc(prm, p.head_dim, status + kTileWord, st);
+    if (rc == CA_OK) return launch_window_ref(prm, p.head_dim, p.dtype, st);
+    if (rc != CA_ERR_UNSUPPORTED) return rc;
+    prm.redo = nullptr;                         // strides of a broadcast: on the CUDA cores
+  }
   return launch_window_ref(prm, p.head_dim, p.dtype, st);
 }
 

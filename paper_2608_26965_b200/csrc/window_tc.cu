@@ -1,0 +1,596 @@
+// Attention over a sliding window on the sm_100a tensor cores.
+//
+// A CTA (one per SM, persistent) works on 256 query rows of a head at a time, two tiles of 128, which share the key and
+// value tiles of 128 rows that they see: the first tokens' tiles, then the window's.  For each of the two and every key tile
+//     S  = Q K^T           tcgen05.mma, Q and K in shared memory
+//     P  = exp2(S c - m)   one query row per thread, so that maximum and sum need no other thread; P goes back over S in
+//                          tensor memory as bf16
+//     O += P V             tcgen05.mma, P from tensor memory
+// and while four warps are at the softmax of one tile, the tensor core is at the products of the other.  Roles: warp 0 loads (TMA, 128-byte
+// swizzle), one thread of warp 1 issues the products, warp 2 sets value rows behind the last key to zero, warp 3 hands out work,
+// warps 4-7 and 8-11 are the softmax of the two query tiles.  All of them run ahead of one another across pieces of work.
+//
+// m is the running maximum, moved only when the new one is 2^8 larger: until then P is at most 2^8 and nothing
+// needs rescaling (P is bf16, O and the sum are fp32: no precision is lost).
+// Masks: only key tiles at a border of a row's window are masked, by selecting scores before the maximum.  A masked P is 0, and
+// 0 x infinity is not: rows whose result is not finite are marked and computed again on the CUDA cores, where
+// what is masked takes no part and no P is above 1 (a second launch, which ends at once when no row is marked).
+#include <math.h>
+
+#include "tc_ptx.cuh"
+#include "window.cuh"
+
+namespace ca {
+
+using namespace ptx;
+
+constexpr int kWtThreads = 384;
+constexpr int kWtRows = kWindowBlock;      // query rows of a piece of work
+constexpr int kWtKeys = 128;
+constexpr float kWtRaise = 8.f;            // log2 units that a row's scores may climb above its reference
+
+template <int D>
+struct WtCfg {
+  static constexpr int PANELS = D / 64;                       // 128-byte wide column panels of a tile
+  static constexpr int PANEL_BYTES = 128 * 128;
+  static constexpr int TILE_BYTES = PANELS * PANEL_BYTES;     // 128 rows
+  static constexpr int NK = D == 128 ? 2 : 4, NV = D == 128 ? 3 : 4;
+  static constexpr int OFF_Q = 0, OFF_K = 2 * TILE_BYTES, OFF_V = OFF_K + NK * TILE_BYTES;
+  static constexpr int OFF_WORK = OFF_V + NV * TILE_BYTES;    // [2] Work
+  static constexpr int OFF_BAR = OFF_WORK + 2 * 64;
+  static constexpr int NUM_BARS = 4 + 4 + 2 * NK + 3 * NV + 10;
+  static constexpr int OFF_MISC = OFF_BAR + 8 * NUM_BARS;     // tensor memory base, abort flag
+  static constexpr int SMEM = 1024 + OFF_MISC + 16;
+  static_assert(SMEM <= 227 * 1024, "shared memory");
+};
+
+// 256 query rows, as the warps read them.  Key tiles: [0, sink_tiles), then from tile_lo on, `tiles` in all.
+struct Work {
+  int b, h, r0, len_q, len_k, tiles, sink_tiles, tile_lo;
+  int lo[2], hi[2];                        // keys that the rows of a query tile see: [lo, hi) and those below sinks
+  int pad[4];
+  __device__ __forceinline__ int tile(int u) const { return u < sink_tiles ? u : tile_lo + u - sink_tiles; }
+  // whether query tile i takes part in the step of key tile t
+  __device__ __forceinline__ bool active(int i, int t, int sinks) const { return takes_part(lo[i], hi[i], t, sinks); }
+  __device__ __forceinline__ static bool takes_part(int lo, int hi, int t, int sinks) {
+    const int k0 = t * kWtKeys;
+    return k0 < hi && (k0 + kWtKeys > lo || k0 < sinks);
+  }
+};
+static_assert(sizeof(Work) == 64, "a work slot");
+
+struct WtParams {
+  WindowParams w;
+  int* next;                               // counter that hands out work, zero at the start
+  int blocks, n_work;                      // pieces of a head, of the call
+  long long wait_limit;
+};
+
+__device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map, int x, int y, int z, int w, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
+      ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(w), "r"(bar)
+      : "memory");
+}
+
+template <int D>
+__global__ void __launch_bounds__(kWtThreads, 1)
+window_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
+                 const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ WtParams prm) {
+  wait_for_previous();
+  using C = WtCfg<D>;
+  extern __shared__ unsigned char smem_unaligned[];
+  unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_unaligned) + 1023) & ~uintptr_t(1023));
+  const uint32_t s_base = smem_u32(smem);
+  const uint32_t s_q = s_base + C::OFF_Q, s_k = s_base + C::OFF_K, s_v = s_base + C::OFF_V;
+  volatile Work* work_ring = reinterpret_cast<volatile Work*>(smem + C::OFF_WORK);
+  const uint32_t bar0 = s_base + C::OFF_BAR;
+  auto b_work_full = [&](int i) { return bar0 + 8 * i; };
+  auto b_work_empty = [&](int i) { return bar0 + 16 + 8 * i; };
+  auto b_q_full = [&](int i) { return bar0 + 32 + 8 * i; };
+  auto b_q_empty = [&](int i) { return bar0 + 48 + 8 * i; };
+  auto b_s_full = [&](int i) { return bar0 + 64 + 8 * i; };
+  auto b_p_ready = [&](int i) { return bar0 + 80 + 8 * i; };
+  auto b_pv_done = [&](int i) { return bar0 + 96 + 8 * i; };
+  auto b_o_full = [&](int i) { return bar0 + 112 + 8 * i; };
+  auto b_o_empty = [&](int i) { return bar0 + 128 + 8 * i; };
+  const uint32_t bar1 = bar0 + 144;
+  auto b_k_full = [&](int s) { return bar1 + 8 * s; };
+  auto b_k_empty = [&](int s) { return bar1 + 8 * (C::NK + s); };
+  auto b_v_full = [&](int s) { return bar1 + 8 * (2 * C::NK + s); };
+  auto b_v_ready = [&](int s) { return bar1 + 8 * (2 * C::NK + C::NV + s); };
+  auto b_v_empty = [&](int s) { return bar1 + 8 * (2 * C::NK + 2 * C::NV + s); };
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + C::OFF_MISC);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + C::OFF_MISC + 4);
+  const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
+  const int sinks = prm.w.sinks;
+
+  if (tid == 0) {
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(b_work_full(i), 1);
+      mbar_init(b_work_empty(i), 11);
+      mbar_init(b_q_full(i), 1);
+      mbar_init(b_q_empty(i), 1);
+      mbar_init(b_s_full(i), 1);
+      mbar_init(b_p_ready(i), 4);
+      mbar_init(b_pv_done(i), 1);
+      mbar_init(b_o_full(i), 1);
+      mbar_init(b_o_empty(i), 4);
+    }
+    for (int s = 0; s < C::NK; ++s) { mbar_init(b_k_full(s), 1); mbar_init(b_k_empty(s), 1); }
+    for (int s = 0; s < C::NV; ++s) { mbar_init(b_v_full(s), 1); mbar_init(b_v_ready(s), 1); mbar_init(b_v_empty(s), 1); }
+    *abort_flag = 0;
+    fence_mbar_init();
+  }
+  if (warp == 1) {
+    tmem_alloc(smem_u32(tmem_slot), 512);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem_base = __shfl_sync(0xffffffffu, *tmem_slot, 0);
+  auto tmem_s = [&](int i) { return tmem_base + i * kWtKeys; };
+  auto tmem_o = [&](int i) { return tmem_base + 2 * kWtKeys + i * 128; };
+
+  auto wait = [&](uint32_t bar, uint32_t phase) { return mbar_wait(bar, phase & 1, abort_flag, prm.w.status, prm.wait_limit); };
+  auto relaxed = [&](uint32_t bar, uint32_t phase) { return mbar_wait_relaxed(bar, phase & 1, abort_flag, prm.w.status, prm.wait_limit); };
+  auto read_work = [&](int n, Work& w) {               // a thread's copy of piece n, which is there
+    const volatile int* src = reinterpret_cast<const volatile int*>(work_ring + (n & 1));
+    int* dst = reinterpret_cast<int*>(&w);
+#pragma unroll
+    for (int i = 0; i < 12; ++i) dst[i] = src[i];
+  };
+
+  if (warp == 3) {
+    // ---------------------------------------------------------- work
+    if (lane == 0) {
+      int n = 0;
+      for (int idx = blockIdx.x;;) {
+        Work w;
+        w.b = -1;
+        if (idx < prm.n_work) {
+          const int rb = idx % prm.blocks, bh = idx / prm.blocks;
+          w.b = bh / prm.w.heads_q;
+          w.h = bh % prm.w.heads_q;
+          w.r0 = rb * kWtRows;
+          const WindowItem it(prm.w, w.b);
+          w.len_q = it.len_q;
+          w.len_k = it.len_k;
+          idx = (int)gridDim.x + atomicAdd(prm.next, 1);
+          if (w.r0 >= it.len_q) continue;
+          const WindowSpan all(prm.w, it, w.r0, min(w.r0 + kWtRows, it.len_q), kWtKeys);
+          w.tiles = all.tiles;
+          w.sink_tiles = all.sink_tiles;
+          w.tile_lo = all.tile_lo;
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const int first = w.r0 + i * kWindowTile;
+            w.lo[i] = w.hi[i] = 0;
+            if (first < it.len_q) {
+              const WindowSpan part(prm.w, it, first, min(first + kWindowTile, it.len_q), kWtKeys);
+              w.lo[i] = part.lo;
+              w.hi[i] = part.hi;
+            }
+          }
+        }
+        if (n >= 2 && !relaxed(b_work_empty(n & 1), (n >> 1) - 1)) break;
+        volatile int* dst = reinterpret_cast<volatile int*>(work_ring + (n & 1));
+        const int* src = reinterpret_cast<const int*>(&w);
+#pragma unroll
+        for (int i = 0; i < 12; ++i) dst[i] = src[i];
+        mbar_arrive(b_work_full(n & 1));
+        ++n;
+        if (w.b < 0) break;
+      }
+    }
+  } else if (warp == 0) {
+    // ---------------------------------------------------------- loads
+    if (lane == 0) {
+      prefetch_tensormap(&tm_q);
+      prefetch_tensormap(&tm_k);
+      prefetch_tensormap(&tm_v);
+      int q_used[2] = {0, 0}, k_slot = 0, v_slot = 0, steps = 0;
+      uint32_t k_ph = 1, v_ph = 1;
+      bool ok = true;
+      for (int n = 0; ok; ++n) {
+        if (!relaxed(b_work_full(n & 1), n >> 1)) break;
+        Work w;
+        read_work(n, w);
+        mbar_arrive(b_work_empty(n & 1));
+        if (w.b < 0) break;
+        const int g = w.h / prm.w.group;
+        bool q_there[2] = {false, false};
+        for (int u = 0; u < w.tiles && ok; ++u) {
+          const int t = w.tile(u);
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            if (!q_there[i] && w.active(i, t, sinks)) {
+              q_there[i] = true;
+              if (q_used[i] > 0) ok = ok && relaxed(b_q_empty(i), q_used[i] - 1);
+              if (!ok) break;
+              ++q_used[i];
+              mbar_expect_tx(b_q_full(i), C::TILE_BYTES);
+#pragma unroll
+              for (int pn = 0; pn < C::PANELS; ++pn)
+                tma_load_4d(s_q + i * C::TILE_BYTES + pn * C::PANEL_BYTES, &tm_q, pn * 64, w.r0 + i * kWindowTile, w.h, w.b, b_q_full(i));
+            }
+          }
+          if (!ok) break;
+          if (steps >= C::NK && !relaxed(b_k_empty(k_slot), k_ph)) { ok = false; break; }
+          mbar_expect_tx(b_k_full(k_slot), C::TILE_BYTES);
+#pragma unroll
+          for (int pn = 0; pn < C::PANELS; ++pn)
+            tma_load_4d(s_k + k_slot * C::TILE_BYTES + pn * C::PANEL_BYTES, &tm_k, pn * 64, t * kWtKeys, g, w.b, b_k_full(k_slot));
+          if (++k_slot == C::NK) { k_slot = 0; k_ph ^= 1; }
+          if (steps >= C::NV && !relaxed(b_v_empty(v_slot), v_ph)) { ok = false; break; }
+          mbar_expect_tx(b_v_full(v_slot), C::TILE_BYTES);
+#pragma unroll
+          for (int pn = 0; pn < C::PANELS; ++pn)
+            tma_load_4d(s_v + v_slot * C::TILE_BYTES + pn * C::PANEL_BYTES, &tm_v, pn * 64, t * kWtKeys, g, w.b, b_v_full(v_slot));
+          if (++v_slot == C::NV) { v_slot = 0; v_ph ^= 1; }
+          ++steps;
+        }
+      }
+    }
+  } else if (warp == 2) {
+    // ---------------------------------------------------------- value rows behind the last key
+    int slot = 0;
+    uint32_t ph = 0;
+    bool ok = true;
+    for (int n = 0; ok; ++n) {
+      ok = __all_sync(0xffffffffu, relaxed(b_work_full(n & 1), n >> 1));
+      if (!ok) break;
+      Work w;
+      read_work(n, w);
+      __syncwarp();
+      if (lane == 0) mbar_arrive(b_work_empty(n & 1));
+      if (w.b < 0) break;
+      for (int u = 0; u < w.tiles; ++u) {
+        ok = __all_sync(0xffffffffu, relaxed(b_v_full(slot), ph));
+        if (!ok) break;
+        const int from = w.len_k - w.tile(u) * kWtKeys;      // rows of the tile from here on are not keys
+        if (from < kWtKeys) {
+          unsigned char* tile = smem + C::OFF_V + slot * C::TILE_BYTES;
+          for (int i = lane; i < C::PANELS * (kWtKeys - from) * 8; i += 32) {
+            const int pn = i / ((kWtKeys - from) * 8), rest = i % ((kWtKeys - from) * 8);
+            *reinterpret_cast<uint4*>(tile + pn * C::PANEL_BYTES + from * 128 + rest * 16) = make_uint4(0u, 0u, 0u, 0u);
+          }
+          fence_proxy_async();
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(b_v_ready(slot));
+        if (++slot == C::NV) { slot = 0; ph ^= 1; }
+      }
+    }
+  } else if (warp == 1) {
+    // ---------------------------------------------------------- products
+    if (elect_one()) {
+      constexpr uint32_t idesc_qk = idesc_bf16_f32(kWindowTile, kWtKeys, 0, 0);
+      constexpr uint32_t idesc_pv = idesc_bf16_f32(kWindowTile, D, 0, 1);
+      const uint64_t q_desc0 = smem_desc_sw128(s_q, 16, 1024);
+      const uint64_t k_desc0 = smem_desc_sw128(s_k, 16, 1024);
+      const uint64_t v_desc0 = smem_desc_sw128(s_v, C::PANEL_BYTES, 1024);
+      int n_s[2] = {0, 0}, n_pv[2] = {0, 0}, n_q[2] = {0, 0}, n_o[2] = {0, 0};   // steps, steps, query tiles, results so far
+      int k_slot = 0, v_slot = 0;
+      uint32_t k_ph = 0, v_ph = 0;
+      bool on[2] = {false, false};             // the step before: query tiles that take part, the first, the last of their steps
+      bool was_first[2] = {false, false}, was_last[2] = {false, false};
+      bool any_before = false;
+      bool ok = true, more = true;
+      Work w;
+      w.tiles = 0;
+      int u = 0, n = 0;
+      bool begun[2] = {false, false};
+      while (ok) {
+        // the step that comes: the next key tile of this piece of work or the first one of the next
+        while (more && u >= w.tiles) {
+          if (!wait(b_work_full(n & 1), n >> 1)) { ok = false; break; }
+          read_work(n, w);
+          mbar_arrive(b_work_empty(n & 1));
+          ++n;
+          u = 0;
+          begun[0] = begun[1] = false;
+          if (w.b < 0) { more = false; w.tiles = 0; }
+        }
+        if (!ok || (!more && !any_before)) break;
+        const int t = more ? w.tile(u) : 0;
+        bool now[2], first[2], last[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          now[i] = more && w.active(i, t, sinks);
+          first[i] = now[i] && !begun[i];
+          begun[i] = begun[i] || now[i];
+          last[i] = now[i] && (t + 1) * kWtKeys >= w.hi[i];  // a query tile's steps end with its window
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          if (on[i]) {
+            // O of query tile i += P V of the step before
+            if (!wait(b_p_ready(i), n_pv[i])) { ok = false; break; }
+            if (!wait(b_v_ready(v_slot), v_ph)) { ok = false; break; }
+            if (was_first[i]) {
+              if (n_o[i] > 0 && !wait(b_o_empty(i), n_o[i] - 1)) { ok = false; break; }
+              ++n_o[i];
+            }
+            tc_fence_after();
+            const uint64_t vd = v_desc0 + ((v_slot * C::TILE_BYTES) >> 4);
+#pragma unroll
+            for (int ks = 0; ks < 8; ++ks)
+              mma_ts(tmem_o(i), tmem_s(i) + ks * 8, vd + (uint64_t)(ks * (2048 >> 4)), idesc_pv, (ks > 0 || !was_first[i]) ? 1u : 0u);
+            mma_commit(b_pv_done(i));
+            if (was_last[i]) mma_commit(b_o_full(i));
+            ++n_pv[i];
+          }
+          if (i == 1 && any_before) {
+            mma_commit(b_v_empty(v_slot));
+            if (++v_slot == C::NV) { v_slot = 0; v_ph ^= 1; }
+          }
+          if (now[i]) {
+            if (first[i]) {
+              if (!wait(b_q_full(i), n_q[i])) { ok = false; break; }
+              ++n_q[i];
+            }
+            if (!wait(b_k_full(k_slot), k_ph)) { ok = false; break; }
+            tc_fence_after();
+            const uint64_t qd = q_desc0 + ((i * C::TILE_BYTES) >> 4), kd = k_desc0 + ((k_slot * C::TILE_BYTES) >> 4);
+#pragma unroll
+            for (int ks = 0; ks < D / 16; ++ks) {
+              const uint32_t off = ((ks / 4) * C::PANEL_BYTES + (ks % 4) * 32) >> 4;
+              mma_ss(tmem_s(i), qd + off, kd + off, idesc_qk, ks > 0 ? 1u : 0u);
+            }
+            mma_commit(b_s_full(i));
+            if (last[i]) mma_commit(b_q_empty(i));
+            ++n_s[i];
+          }
+        }
+        if (!ok) break;
+        if (more) {
+          mma_commit(b_k_empty(k_slot));
+          if (++k_slot == C::NK) { k_slot = 0; k_ph ^= 1; }
+          ++u;
+        }
+        any_before = more;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) { on[i] = now[i]; was_first[i] = first[i]; was_last[i] = last[i]; }
+      }
+    }
+    __syncwarp();
+  } else {
+    // ---------------------------------------------------------- softmax and results
+    const int i = (warp >> 2) - 1, quarter = warp & 3;
+    const int row = quarter * 32 + lane;
+    const uint32_t lane_addr = (uint32_t)(quarter * 32) << 16;
+    const uint32_t t_s = tmem_s(i) + lane_addr, t_o = tmem_o(i) + lane_addr;
+    const float scale = prm.w.scale_log2;
+    auto all_wait = [&](uint32_t bar, uint32_t phase) { return __all_sync(0xffffffffu, wait(bar, phase)); };
+    int steps = 0, results = 0;
+    bool ok = true;
+    for (int n = 0; ok; ++n) {
+      ok = all_wait(b_work_full(n & 1), n >> 1);
+      if (!ok) break;
+      Work w;
+      read_work(n, w);
+      __syncwarp();
+      if (lane == 0) mbar_arrive(b_work_empty(n & 1));
+      if (w.b < 0) break;
+      const int r = w.r0 + i * kWindowTile + row;            // query row
+      if (w.r0 + i * kWindowTile >= w.len_q) continue;
+      const WindowItem it(w.len_q, w.len_k);
+      const WindowSpan span(prm.w, it, w.r0 + i * kWindowTile, min(w.r0 + (i + 1) * kWindowTile, w.len_q), kWtKeys);
+      const WindowRow sees(prm.w, it, r);
+      const int lo = i == 0 ? w.lo[0] : w.lo[1], hi = i == 0 ? w.hi[0] : w.hi[1];
+      float m = -INFINITY, l = 0.f;
+      bool begun = false;
+#pragma unroll 1
+      for (int u = 0; u < w.tiles; ++u) {
+        const int t = w.tile(u), j0 = t * kWtKeys;
+        if (!Work::takes_part(lo, hi, t, sinks)) continue;
+        ok = all_wait(b_s_full(i), steps);
+        if (!ok) break;
+        tc_fence_after();
+        uint32_t s[4][32];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) tmem_ld32(t_s + c * 32, s[c]);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) tmem_wait_ld32(s[c]);
+        if (!span.whole(j0, j0 + kWtKeys)) {
+          // columns below `end`, and from `from` on or below `sink`
+          const int end = sees.end - j0, from = sees.from - j0, sink = sinks - j0;
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            auto below = [&](int x) {                        // bits of columns below x
+              const int k = x - c * 32;
+              return k >= 32 ? 0xffffffffu : k <= 0 ? 0u : (1u << k) - 1u;
+            };
+            const unsigned seen = below(end) & (~below(from) | below(sink));
+#pragma unroll
+            for (int e = 0; e < 32; ++e)
+              if (!((seen >> e) & 1u)) s[c][e] = 0xff800000u;
+          }
+        }
+        // ---- maximum, reference
+        float top = -INFINITY;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          float x0 = -INFINITY, x1 = -INFINITY;
+#pragma unroll
+          for (int e = 0; e < 32; e += 4) {
+            x0 = max3(x0, __uint_as_float(s[c][e]), __uint_as_float(s[c][e + 1]));
+            x1 = max3(x1, __uint_as_float(s[c][e + 2]), __uint_as_float(s[c][e + 3]));
+          }
+          top = max3(top, x0, x1);
+        }
+        top *= scale;
+        const bool raise = top > m + kWtRaise || (m == -INFINITY && top > -INFINITY);
+        if (__any_sync(0xffffffffu, raise)) {
+          const float up = raise ? top : m;
+          const float by = m == -INFINITY ? 0.f : ex2_approx(m - up);
+          l *= by;
+          m = up;
+          if (begun) {
+            // the products of the step before are complete; those of this step wait for this warp
+            ok = all_wait(b_pv_done(i), steps - 1);
+            if (!ok) break;
+            tc_fence_after();
+#pragma unroll 1
+            for (int c = 0; c < D / 16; ++c) {
+              uint32_t o[16];
+              tmem_ld16(t_o + c * 16, o);
+              tmem_wait_ld();
+#pragma unroll
+              for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * by);
+              tmem_st16(t_o + c * 16, o);
+            }
+          }
+        }
+        // ---- probabilities: column c to half a word
+        const float ref = m == -INFINITY ? 0.f : -m;
+        const f32x2 sc2 = pack2(scale, scale), nm2 = pack2(ref, ref);
+        f32x2 sum0 = pack2(0.f, 0.f), sum1 = sum0;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          uint32_t pk[16];
+#pragma unroll
+          for (int e = 0; e < 32; e += 4) {
+            float x0, x1, x2, x3;
+            unpack2(fma2(pack2(__uint_as_float(s[c][e]), __uint_as_float(s[c][e + 1])), sc2, nm2), x0, x1);
+            unpack2(fma2(pack2(__uint_as_float(s[c][e + 2]), __uint_as_float(s[c][e + 3])), sc2, nm2), x2, x3);
+            x0 = ex2_approx(x0); x1 = ex2_approx(x1); x2 = ex2_approx(x2); x3 = ex2_approx(x3);
+            sum0 = add2(sum0, pack2(x0, x1));
+            sum1 = add2(sum1, pack2(x2, x3));
+            pk[e / 2] = pack_bf16x2(x0, x1);
+            pk[e / 2 + 1] = pack_bf16x2(x2, x3);
+          }
+          tmem_st16(t_s + c * 16, pk);
+        }
+        tmem_wait_st();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(b_p_ready(i));
+        float a0, a1, a2, a3;
+        unpack2(sum0, a0, a1);
+        unpack2(sum1, a2, a3);
+        l += (a0 + a1) + (a2 + a3);
+        begun = true;
+        ++steps;
+      }
+      if (!ok) break;
+      // ---- O / l; a row that sees nothing: zeros, log-sum-exp -inf
+      const bool live = r < w.len_q, empty = l == 0.f;
+      const float inv = empty ? 0.f : 1.f / l;
+      __nv_bfloat16* out = static_cast<__nv_bfloat16*>(prm.w.o) + w.b * prm.w.o_b + w.h * prm.w.o_h + r * prm.w.o_n;
+      float any = 0.f;
+      if (begun) {
+        ok = all_wait(b_o_full(i), results);
+        if (!ok) break;
+        ++results;
+        tc_fence_after();
+      }
+#pragma unroll 1
+      for (int c = 0; c < D / 32; ++c) {
+        uint32_t o[32];
+#pragma unroll
+        for (int e = 0; e < 32; ++e) o[e] = 0u;
+        if (begun) {
+          tmem_ld32(t_o + c * 32, o);
+          tmem_wait_ld32(o);
+        }
+#pragma unroll
+        for (int e = 0; e < 32; ++e) any += __uint_as_float(o[e]);
+        if (live) {
+          uint4* dst = reinterpret_cast<uint4*>(out + c * 32);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            uint4 x;
+            x.x = pack_bf16x2(__uint_as_float(o[8 * e + 0]) * inv, __uint_as_float(o[8 * e + 1]) * inv);
+            x.y = pack_bf16x2(__uint_as_float(o[8 * e + 2]) * inv, __uint_as_float(o[8 * e + 3]) * inv);
+            x.z = pack_bf16x2(__uint_as_float(o[8 * e + 4]) * inv, __uint_as_float(o[8 * e + 5]) * inv);
+            x.w = pack_bf16x2(__uint_as_float(o[8 * e + 6]) * inv, __uint_as_float(o[8 * e + 7]) * inv);
+            dst[e] = empty ? make_uint4(0u, 0u, 0u, 0u) : x;
+          }
+        }
+      }
+      if (begun) {
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(b_o_empty(i));
+      }
+      if (live && prm.w.lse)
+        prm.w.lse[((size_t)w.b * prm.w.heads_q + w.h) * prm.w.n_q + r] = empty ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
+      // rows to be computed again: a word for each 32
+      const bool again = __any_sync(0xffffffffu, live && !empty && !(fabsf(any) < INFINITY && l < INFINITY));
+      if (lane == 0) {
+        prm.w.redo[((size_t)(w.b * prm.w.heads_q + w.h) * prm.blocks + w.r0 / kWtRows) * 8 + i * 4 + quarter] = again ? 1 : 0;
+        if (again) atomicExch(prm.w.redo_any, 1);
+      }
+    }
+  }
+  let_next_start();
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 1) tmem_dealloc(tmem_base, 512);
+}
+
+// ---- host side -------------------------------------------------------------------------------------------
+
+typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                                  const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+static EncodeTiledFn encode_fn() {
+  static EncodeTiledFn fn = [] {
+    void* ptr = nullptr;
+    cudaDriverEntryPointQueryResult found;
+    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &ptr, cudaEnableDefault, &found) != cudaSuccess || found != cudaDriverEntryPointSuccess)
+      ptr = nullptr;
+    return reinterpret_cast<EncodeTiledFn>(ptr);
+  }();
+  return fn;
+}
+
+// [batch, heads, rows, D] by strides (elements), boxes of 128 rows by 64 columns
+static bool rows_map(CUtensorMap* map, const void* base, int D, int n, int heads, int batch, long long s_n, long long s_h, long long s_b) {
+  EncodeTiledFn fn = encode_fn();
+  if (!fn) return false;
+  const cuuint64_t dims[4] = {(cuuint64_t)D, (cuuint64_t)n, (cuuint64_t)heads, (cuuint64_t)batch};
+  const long long stride[3] = {n > 1 ? s_n : D, heads > 1 ? s_h : D, batch > 1 ? s_b : D};
+  cuuint64_t strides[3];
+  for (int i = 0; i < 3; ++i) {
+    if (stride[i] <= 0 || stride[i] >= (1LL << 39)) return false;    // 40 bits of bytes; a broadcast dimension has none
+    strides[i] = (cuuint64_t)stride[i] * 2;
+  }
+  const cuuint32_t box[4] = {64, 128, 1, 1}, step[4] = {1, 1, 1, 1};
+  return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int D>
+static int launch_window_tc_d(const CUtensorMap* maps, const WtParams& prm, LaunchStream st) {
+  auto kernel = window_tc_kernel<D>;
+  int dev = 0, sms = 0;
+  CA_RETURN_IF_CUDA(cudaGetDevice(&dev));
+  CA_RETURN_IF_CUDA(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
+  CA_RETURN_IF_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, WtCfg<D>::SMEM));
+  launch_chained(kernel, prm.n_work < sms ? prm.n_work : sms, kWtThreads, WtCfg<D>::SMEM, st, maps[0], maps[1], maps[2], prm);
+  CA_LAUNCH_CHECK();
+  return CA_OK;
+}
+
+// CA_ERR_UNSUPPORTED: strides that a tensor map does not describe
+int launch_window_tc(const WindowParams& w, int D, int* next, LaunchStream st) {
+  CUtensorMap maps[3];
+  if (!rows_map(&maps[0], w.q, D, w.n_q, w.heads_q, w.batch, w.q_n, w.q_h, w.q_b) ||
+      !rows_map(&maps[1], w.k, D, w.n_k, w.heads_kv, w.batch, w.k_n, w.k_h, w.k_b) ||
+      !rows_map(&maps[2], w.v, D, w.n_k, w.heads_kv, w.batch, w.v_n, w.v_h, w.v_b))
+    return CA_ERR_UNSUPPORTED;
+  WtParams prm{};
+  prm.w = w;
+  prm.next = next;
+  prm.blocks = ceil_div(w.n_q, kWtRows);
+  if ((long long)prm.blocks * w.heads_q * w.batch > 0x3fffffffLL) return CA_ERR_UNSUPPORTED;
+  prm.n_work = prm.blocks * w.heads_q * w.batch;
+  prm.wait_limit = kWaitLimitCycles;
+  CA_RETURN_IF_CUDA(cudaMemsetAsync(w.status, 0, kStatusBytes, st));
+  return D == 64 ? launch_window_tc_d<64>(maps, prm, st) : launch_window_tc_d<128>(maps, prm, st);
+}
+
+}  // namespace ca

@@ -161,8 +161,11 @@ def test_values_that_are_not_numbers_outside_the_window(dtype, flags, d):
     want, l64, bound, lb, empty = ref.attend(q[0, 0].double(), k[0, 0].double(), v[0, 0].double(), see, 1 / math.sqrt(d), DT[dtype],
                                              dtype == "bf16" and not flags)
     ref.check(O[0, 0, rest], want[rest], bound[rest], "rows that do not see them")
-    # a value that is not a number leaves the weights as they are
-    assert torch.equal(lse[0, 0, ~sees(220)], clean[1][0, 0, ~sees(220)])
+    # A value that is not a number leaves the weights as they are.  (The rows that see it may come from another kernel, whose sums have
+    # another order: each is within its bound of the 64-bit value, so the two are within twice that.)
+    _, _, _, lb, _ = ref.attend(q[0, 0].double(), k[0, 0].double(), v[0, 0].double(), ref.window_mask(n, n, 30, 5, 2, DEV), 1 / math.sqrt(d), DT[dtype],
+                                dtype == "bf16" and not flags)
+    ref.check(lse[0, 0, ~sees(220)], clean[1][0, 0, ~sees(220)].double(), 2 * lb[~sees(220)], "log-sum-exp")
     assert torch.isnan(lse[0, 0, sees(220)]).all()
 
 
