@@ -11,7 +11,7 @@ struct WindowParams {
   float* lse;                       // [batch][heads_q][n_q] or null
   const int32_t *len_q, *len_k;     // [batch] or null
   int* status;
-  int32_t* redo;                    // [batch * heads_q][blocks of kWindowBlock rows][8]: rows 32 at a time to compute again (null: all)
+  int32_t* redo;                    // [batch * heads_q][blocks of kWindowBlock rows][16]: two words for 32 rows, to be computed again if one is set (null: all)
   int32_t* redo_any;                // whether there are any
   int batch, heads_q, heads_kv, group, n_q, n_k, left, right, sinks;
   float scale_log2;

@@ -53,8 +53,8 @@ __global__ void __launch_bounds__(kWrThreads) window_ref_kernel(const __grid_con
   const WindowItem it(prm, b);
   if (r0 >= it.len_q) continue;
   if (prm.redo) {
-    const int32_t* marks = prm.redo + ((size_t)bh * ((prm.n_q + kWindowBlock - 1) / kWindowBlock) + r0 / kWindowBlock) * 8 + r0 % kWindowBlock / 32;
-    if (marks[0] == 0 && marks[1] == 0) continue;
+    const int32_t* marks = prm.redo + ((size_t)bh * ((prm.n_q + kWindowBlock - 1) / kWindowBlock) + r0 / kWindowBlock) * 16 + r0 % kWindowBlock / 16;
+    if ((marks[0] | marks[1] | marks[2] | marks[3]) == 0) continue;
   }
   const int rows = min(kWrRows, it.len_q - r0);
   const WindowSpan span(prm, it, r0, r0 + rows, kWrKeys);
@@ -191,7 +191,7 @@ int launch_window_ref(const WindowParams& prm, int D, int dtype, LaunchStream st
 
 size_t window_workspace_bytes(const ca_window_t& p) {
   // status block, marks of the rows to compute again
-  return kStatusBytes + align_up((size_t)p.batch * p.heads_q * ceil_div(p.n_q, kWindowBlock) * 8 * sizeof(int32_t), 256);
+  return kStatusBytes + align_up((size_t)p.batch * p.heads_q * ceil_div(p.n_q, kWindowBlock) * 16 * sizeof(int32_t), 256);
 }
 
 int launch_window(const ca_window_t& p, const ca_rows_t* Q, const ca_rows_t* K, const ca_rows_t* V, const int32_t* len_q,

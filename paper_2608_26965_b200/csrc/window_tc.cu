@@ -27,6 +27,11 @@ using namespace ptx;
 constexpr int kWtThreads = 384;
 constexpr int kWtRows = kWindowBlock;      // query rows of a piece of work
 constexpr int kWtKeys = 128;
+
+
+
+constexpr int kWtEvery = 8;                // one pair of columns in eight takes its exponentials from the FMA units
+constexpr float kE1 = 0.693147004f, kE2 = 0.240222424f, kE3 = 0.0555073358f, kE4 = 0.00967151299f, kE5 = 0.00132647273f;
 constexpr float kWtRaise = 8.f;            // log2 units that a row's scores may climb above its reference
 
 template <int D>
@@ -38,7 +43,7 @@ struct WtCfg {
   static constexpr int OFF_Q = 0, OFF_K = 2 * TILE_BYTES, OFF_V = OFF_K + NK * TILE_BYTES;
   static constexpr int OFF_WORK = OFF_V + NV * TILE_BYTES;    // [2] Work
   static constexpr int OFF_BAR = OFF_WORK + 2 * 64;
-  static constexpr int NUM_BARS = 4 + 4 + 2 * NK + 3 * NV + 10;
+  static constexpr int NUM_BARS = 20 + 2 * NK + 3 * NV;
   static constexpr int OFF_MISC = OFF_BAR + 8 * NUM_BARS;     // tensor memory base, abort flag
   static constexpr int SMEM = 1024 + OFF_MISC + 16;
   static_assert(SMEM <= 227 * 1024, "shared memory");
@@ -73,6 +78,34 @@ __device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map
       : "memory");
 }
 
+__device__ __forceinline__ f32x2 exp2_unit(f32x2 x) {
+  float a, b;
+  unpack2(x, a, b);
+  return pack2(ex2_approx(a), ex2_approx(b));
+}
+// 2^x without the special-function unit, for part of the scores (kWtEvery): x = j + f with j the nearest whole number, 2^f by a
+// polynomial of degree 5 (fitted to the smallest relative error on [-1/2, 1/2] with the constant term 1; 1.2e-7 with its roundings)
+// and j added to the exponent.  x at or below -127 gives exactly 0 (there the polynomial is 1, whose exponent field is 127), above 127 about 2^127,
+// which makes the sum leave the range as infinity would.
+__device__ __forceinline__ f32x2 exp2_fma(f32x2 x) {
+  float a, b;
+  unpack2(x, a, b);
+  x = pack2(fminf(fmaxf(a, -127.f), 127.f), fminf(fmaxf(b, -127.f), 127.f));
+  const f32x2 magic = pack2(12582912.f, 12582912.f), magic_neg = pack2(-12582912.f, -12582912.f);   // 1.5 2^23: j in the low bits
+  const f32x2 shifted = add2(x, magic);
+  const f32x2 f = fma2(add2(shifted, magic_neg), pack2(-1.f, -1.f), x);
+  f32x2 p = pack2(kE5, kE5);
+  p = fma2(p, f, pack2(kE4, kE4));
+  p = fma2(p, f, pack2(kE3, kE3));
+  p = fma2(p, f, pack2(kE2, kE2));
+  p = fma2(p, f, pack2(kE1, kE1));
+  p = fma2(p, f, pack2(1.f, 1.f));
+  float pa, pb, ja, jb;
+  unpack2(p, pa, pb);
+  unpack2(shifted, ja, jb);
+  return pack2(__int_as_float(__float_as_int(pa) + (__float_as_int(ja) << 23)), __int_as_float(__float_as_int(pb) + (__float_as_int(jb) << 23)));
+}
+
 template <int D>
 __global__ void __launch_bounds__(kWtThreads, 1)
 window_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
@@ -94,7 +127,8 @@ window_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
   auto b_pv_done = [&](int i) { return bar0 + 96 + 8 * i; };
   auto b_o_full = [&](int i) { return bar0 + 112 + 8 * i; };
   auto b_o_empty = [&](int i) { return bar0 + 128 + 8 * i; };
-  const uint32_t bar1 = bar0 + 144;
+  auto b_p_half = [&](int i) { return bar0 + 144 + 8 * i; };
+  const uint32_t bar1 = bar0 + 160;
   auto b_k_full = [&](int s) { return bar1 + 8 * s; };
   auto b_k_empty = [&](int s) { return bar1 + 8 * (C::NK + s); };
   auto b_v_full = [&](int s) { return bar1 + 8 * (2 * C::NK + s); };
@@ -112,6 +146,7 @@ window_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
       mbar_init(b_q_full(i), 1);
       mbar_init(b_q_empty(i), 1);
       mbar_init(b_s_full(i), 1);
+      mbar_init(b_p_half(i), 4);
       mbar_init(b_p_ready(i), 4);
       mbar_init(b_pv_done(i), 1);
       mbar_init(b_o_full(i), 1);
@@ -307,7 +342,7 @@ window_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
         for (int i = 0; i < 2; ++i) {
           if (on[i]) {
             // O of query tile i += P V of the step before
-            if (!wait(b_p_ready(i), n_pv[i])) { ok = false; break; }
+            if (!wait(b_p_half(i), n_pv[i])) { ok = false; break; }
             if (!wait(b_v_ready(v_slot), v_ph)) { ok = false; break; }
             if (was_first[i]) {
               if (n_o[i] > 0 && !wait(b_o_empty(i), n_o[i] - 1)) { ok = false; break; }
@@ -316,8 +351,13 @@ window_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
             tc_fence_after();
             const uint64_t vd = v_desc0 + ((v_slot * C::TILE_BYTES) >> 4);
 #pragma unroll
-            for (int ks = 0; ks < 8; ++ks)
+            for (int ks = 0; ks < 4; ++ks)
               mma_ts(tmem_o(i), tmem_s(i) + ks * 8, vd + (uint64_t)(ks * (2048 >> 4)), idesc_pv, (ks > 0 || !was_first[i]) ? 1u : 0u);
+            if (!wait(b_p_ready(i), n_pv[i])) { ok = false; break; }
+            tc_fence_after();
+#pragma unroll
+            for (int ks = 4; ks < 8; ++ks)
+              mma_ts(tmem_o(i), tmem_s(i) + ks * 8, vd + (uint64_t)(ks * (2048 >> 4)), idesc_pv, 1u);
             mma_commit(b_pv_done(i));
             if (was_last[i]) mma_commit(b_o_full(i));
             ++n_pv[i];
@@ -389,38 +429,50 @@ window_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
         ok = all_wait(b_s_full(i), steps);
         if (!ok) break;
         tc_fence_after();
-        uint32_t s[4][32];
-#pragma unroll
-        for (int c = 0; c < 4; ++c) tmem_ld32(t_s + c * 32, s[c]);
-#pragma unroll
-        for (int c = 0; c < 4; ++c) tmem_wait_ld32(s[c]);
-        if (!span.whole(j0, j0 + kWtKeys)) {
-          // columns below `end`, and from `from` on or below `sink`
-          const int end = sees.end - j0, from = sees.from - j0, sink = sinks - j0;
-#pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            auto below = [&](int x) {                        // bits of columns below x
-              const int k = x - c * 32;
-              return k >= 32 ? 0xffffffffu : k <= 0 ? 0u : (1u << k) - 1u;
-            };
-            const unsigned seen = below(end) & (~below(from) | below(sink));
-#pragma unroll
-            for (int e = 0; e < 32; ++e)
-              if (!((seen >> e) & 1u)) s[c][e] = 0xff800000u;
-          }
-        }
-        // ---- maximum, reference
         float top = -INFINITY;
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {
+        uint32_t sa[32], sb[32];
+        auto maximum = [&](const uint32_t (&s)[32]) {
           float x0 = -INFINITY, x1 = -INFINITY;
 #pragma unroll
           for (int e = 0; e < 32; e += 4) {
-            x0 = max3(x0, __uint_as_float(s[c][e]), __uint_as_float(s[c][e + 1]));
-            x1 = max3(x1, __uint_as_float(s[c][e + 2]), __uint_as_float(s[c][e + 3]));
+            x0 = max3(x0, __uint_as_float(s[e]), __uint_as_float(s[e + 1]));
+            x1 = max3(x1, __uint_as_float(s[e + 2]), __uint_as_float(s[e + 3]));
           }
           top = max3(top, x0, x1);
+        };
+        if (span.whole(j0, j0 + kWtKeys)) {
+          tmem_ld32(t_s, sa);
+          tmem_ld32(t_s + 32, sb);
+          tmem_wait_ld32(sa);
+          maximum(sa);
+          tmem_wait_ld32(sb);
+          tmem_ld32(t_s + 64, sa);
+          maximum(sb);
+          tmem_ld32(t_s + 96, sb);
+          tmem_wait_ld32(sa);
+          maximum(sa);
+          tmem_wait_ld32(sb);
+          maximum(sb);
+        } else {
+          const int end = sees.end - j0, from = sees.from - j0, sink = sinks - j0;
+#pragma unroll 1
+          for (int c = 0; c < 128; c += 32) {
+            tmem_ld32(t_s + c, sa);
+            auto below = [&](int x) {
+              const int k = x - c;
+              return k >= 32 ? 0xffffffffu : k <= 0 ? 0u : (1u << k) - 1u;
+            };
+            const unsigned seen = below(end) & (~below(from) | below(sink));
+            tmem_wait_ld32(sa);
+#pragma unroll
+            for (int e = 0; e < 32; ++e)
+              if (!((seen >> e) & 1u)) sa[e] = 0xff800000u;
+            tmem_st32(t_s + c, sa);
+            maximum(sa);
+          }
+          tmem_wait_st();
         }
+        tmem_ld32(t_s, sa);
         top *= scale;
         const bool raise = top > m + kWtRaise || (m == -INFINITY && top > -INFINITY);
         if (__any_sync(0xffffffffu, raise)) {
@@ -429,7 +481,6 @@ window_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
           l *= by;
           m = up;
           if (begun) {
-            // the products of the step before are complete; those of this step wait for this warp
             ok = all_wait(b_pv_done(i), steps - 1);
             if (!ok) break;
             tc_fence_after();
@@ -444,26 +495,42 @@ window_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
             }
           }
         }
-        // ---- probabilities: column c to half a word
         const float ref = m == -INFINITY ? 0.f : -m;
         const f32x2 sc2 = pack2(scale, scale), nm2 = pack2(ref, ref);
         f32x2 sum0 = pack2(0.f, 0.f), sum1 = sum0;
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {
+        auto exponentials = [&](const uint32_t (&s)[32], uint32_t dst) {
           uint32_t pk[16];
 #pragma unroll
           for (int e = 0; e < 32; e += 4) {
+            f32x2 x01 = fma2(pack2(__uint_as_float(s[e]), __uint_as_float(s[e + 1])), sc2, nm2);
+            f32x2 x23 = fma2(pack2(__uint_as_float(s[e + 2]), __uint_as_float(s[e + 3])), sc2, nm2);
+            x01 = e % kWtEvery == 0 ? exp2_fma(x01) : exp2_unit(x01);
+            x23 = exp2_unit(x23);
+            sum0 = add2(sum0, x01);
+            sum1 = add2(sum1, x23);
             float x0, x1, x2, x3;
-            unpack2(fma2(pack2(__uint_as_float(s[c][e]), __uint_as_float(s[c][e + 1])), sc2, nm2), x0, x1);
-            unpack2(fma2(pack2(__uint_as_float(s[c][e + 2]), __uint_as_float(s[c][e + 3])), sc2, nm2), x2, x3);
-            x0 = ex2_approx(x0); x1 = ex2_approx(x1); x2 = ex2_approx(x2); x3 = ex2_approx(x3);
-            sum0 = add2(sum0, pack2(x0, x1));
-            sum1 = add2(sum1, pack2(x2, x3));
+            unpack2(x01, x0, x1);
+            unpack2(x23, x2, x3);
             pk[e / 2] = pack_bf16x2(x0, x1);
             pk[e / 2 + 1] = pack_bf16x2(x2, x3);
           }
-          tmem_st16(t_s + c * 16, pk);
-        }
+          tmem_st16(dst, pk);
+        };
+        tmem_wait_ld32(sa);
+        tmem_ld32(t_s + 32, sb);
+        exponentials(sa, t_s);
+        tmem_wait_ld32(sb);
+        tmem_ld32(t_s + 64, sa);
+        exponentials(sb, t_s + 16);
+        tmem_wait_st();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(b_p_half(i));
+        tmem_wait_ld32(sa);
+        tmem_ld32(t_s + 96, sb);
+        exponentials(sa, t_s + 32);
+        tmem_wait_ld32(sb);
+        exponentials(sb, t_s + 48);
         tmem_wait_st();
         tc_fence_before();
         __syncwarp();
@@ -477,7 +544,7 @@ window_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
       }
       if (!ok) break;
       // ---- O / l; a row that sees nothing: zeros, log-sum-exp -inf
-      const bool live = r < w.len_q, empty = l == 0.f;
+      const bool live = r < w.len_q, empty = l < 0.5f;
       const float inv = empty ? 0.f : 1.f / l;
       __nv_bfloat16* out = static_cast<__nv_bfloat16*>(prm.w.o) + w.b * prm.w.o_b + w.h * prm.w.o_h + r * prm.w.o_n;
       float any = 0.f;
@@ -521,7 +588,7 @@ window_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
       // rows to be computed again: a word for each 32
       const bool again = __any_sync(0xffffffffu, live && !empty && !(fabsf(any) < INFINITY && l < INFINITY));
       if (lane == 0) {
-        prm.w.redo[((size_t)(w.b * prm.w.heads_q + w.h) * prm.blocks + w.r0 / kWtRows) * 8 + i * 4 + quarter] = again ? 1 : 0;
+        prm.w.redo[((size_t)(w.b * prm.w.heads_q + w.h) * prm.blocks + w.r0 / kWtRows) * 16 + (i * 4 + quarter) * 2] = prm.w.redo[((size_t)(w.b * prm.w.heads_q + w.h) * prm.blocks + w.r0 / kWtRows) * 16 + (i * 4 + quarter) * 2 + 1] = again ? 1 : 0;
         if (again) atomicExch(prm.w.redo_any, 1);
       }
     }
