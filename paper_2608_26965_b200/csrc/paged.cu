@@ -3,14 +3,17 @@
 //     j >= n - 1 - left  or  j < sinks.
 //
 // What bounds it: reading every visible key and value row once, at 4 d bytes (bf16) and 4 d operations per row and
-// query head; the query heads of a key head share the read.  So the rows of a tile are those heads (up to 16), and the products run
-// as m16n8k16 (the tcgen05 tiles have 64 rows and more, three quarters of them empty here, and the tensor
-// core is not what is waited for).
+// query head; the query heads of a key head share the read.  So the rows of a tile are those heads, and the products run as m16n8k16
+// (the tcgen05 tiles have 64 rows and more, nine tenths of them empty here, and the tensor core is not what is waited for).
+// A warp's step is a chain of products, softmax and products: it is the length of that chain, and how many warps are on it, that
+// costs bandwidth before memory does (with the query heads as the 16 rows of the product, half of them empty, 623 instructions a
+// step: two sequences of 131,000 rows, 40 heads, 981 us; as its 8 columns 786, 6.8 TB/s).
 //
 // Split: the visible rows of all sequences and key heads are one line of units, which the CTAs cut into equal
-// parts: whatever the lengths, every CTA reads as much as any other.  A part begins and ends anywhere; where a sequence's rows lie in
-// several parts, each leaves {O, m, l} in the workspace, and the CTA that is last to do so joins them, in the
-// order of the rows, so that results do not depend on the order in which CTAs finish.
+// parts: whatever the lengths, every CTA has as much to do as any other.  A part begins and ends anywhere; where a sequence's rows lie in
+// several parts, each leaves {O, m, l} in the workspace, and a last launch joins them in the order of the rows, so that results
+// do not depend on the order in which CTAs finish.  (The last CTA of a sequence joining by itself, while its own part waits, took 59 us
+// instead of 41 for four sequences of up to 60,000 rows and 16 query heads to a key head, and 85 instead of 51.5 for 64 short ones.)
 // A CTA's warps take the rows of a unit in turn and have their own rings of asynchronous copies: nothing but the end of
 // a sequence makes them wait for one another, and copies run ahead across that.  Rows that are not visible are filled with
 // zeros instead of being read, so what stands in them (in unused slots of a page, anything) is not seen.
@@ -27,7 +30,12 @@ using namespace ptx;
 
 constexpr int kPagedWarps = 4;
 constexpr int kPagedThreads = kPagedWarps * 32;
+// What the start and the end of a (sequence, key head, row tile) cost, in units of rows: without it the parts that hold many short
+// sequences take longest (64 sequences of 1 to 8,192 rows, 8 key heads of 4 query heads, d = 128: 0 90 us, 1 61, 2 51.5, 4 53, 8 57).
+constexpr int kPairUnits = 3;
 constexpr int kPagedMaxCtas = 640;           // most CTAs of a launch: the workspace holds two partial results of each
+
+__host__ __device__ inline int ceil_div_device(int a, int b) { return (a + b - 1) / b; }
 
 struct PagedParams {
   const void* q;
@@ -39,8 +47,7 @@ struct PagedParams {
   const int32_t *lengths, *page_table;
   int* status;
   long long* units;              // [batch + 1] units of a (key head, row tile) of the sequences before
-  int* arrived;                  // [batch * heads_kv * row_tiles]
-  float* partial;                // [2 * CTAs][rows][D + 2]: O (not divided), m (log2 units), l
+  float* partial;                // [2 * CTAs] O [rows][D] (not divided), {m (log2 units), l} [rows]; rows (D + 4) floats apart
   int batch, heads_q, heads_kv, group, row_tiles, page_rows, pages, pages_per_sequence, appended, left, sinks;
   float scale_log2;
 };
@@ -61,15 +68,13 @@ struct Span {
   __device__ __forceinline__ bool sees(int j) const { return j < n && (j >= lo || j < sink_end); }
 };
 
-// One CTA: units before each sequence, counters and status cleared, lengths looked at.
+// One CTA: units before each sequence, status cleared, lengths looked at.
 __global__ void __launch_bounds__(1024) paged_plan_kernel(const __grid_constant__ PagedParams prm, int U) {
   wait_for_previous();
   let_next_start();
   __shared__ long long warp_sum[32];
   __shared__ long long carry;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int segments = prm.batch * prm.heads_kv * prm.row_tiles;
-  for (int i = tid; i < segments; i += blockDim.x) prm.arrived[i] = 0;
   int bad = 0;
   if (tid == 0) { carry = 0; prm.units[0] = 0; }
   __syncthreads();
@@ -79,7 +84,7 @@ __global__ void __launch_bounds__(1024) paged_plan_kernel(const __grid_constant_
     if (b < prm.batch) {
       const long long rows = (long long)prm.lengths[b] + prm.appended;
       bad |= rows < 0 || rows > (long long)prm.pages_per_sequence * prm.page_rows;
-      v = Span(prm, b, U).tiles;
+      v = Span(prm, b, U).tiles + kPairUnits;
     }
     for (int d = 1; d < 32; d <<= 1) {
       const long long o = __shfl_up_sync(0xffffffffu, v, d);
@@ -119,185 +124,240 @@ __device__ __forceinline__ void mma16816(float (&c)[4], const uint32_t (&a)[4], 
                : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-__device__ __forceinline__ float max_of_keys(float x) {      // over the four lanes that hold a row's columns
-  x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 1));
-  return fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 2));
-}
-__device__ __forceinline__ float sum_of_keys(float x) {
-  x += __shfl_xor_sync(0xffffffffu, x, 1);
-  return x + __shfl_xor_sync(0xffffffffu, x, 2);
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
+  uint32_t y;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
 }
 
-// Tensor-core products of a warp: 16 query rows against 16 keys at a time.  Accumulator layout of m16n8: a thread holds
-// rows lane/4 and lane/4 + 8, columns 2 (lane % 4) and the next of every 8.
-template <int D>
+// Tensor-core products of a warp, 16 keys at a time, keys (then columns of V) as the rows of the m16n8k16 product and query
+// rows as its columns: eight query heads to a key head are one column tile, and no half of the product is empty.
+//     S^T = K Q^T      a thread holds keys lane/4 and lane/4 + 8, query rows 2 (lane % 4) and the next
+//     O^T += V^T P^T   columns of V lane/4 and lane/4 + 8 of every 16, the same query rows
+// (P^T changes hands inside the warp by 8 x 8 transposes.)
+template <int D, int NT>
 struct WarpMma {
   using T = __nv_bfloat16;
-  static constexpr int ROWS = 16, KEYS = 16;
+  static constexpr int ROWS = 8 * NT, KEYS = 16, STAGES = NT == 1 ? 3 : 2;
   static constexpr int ROW_BYTES = D * 2, CHUNKS = ROW_BYTES / 16;
-  uint32_t q[D / 16][4];
-  float o[D / 8][4];
-  float m[2], l[2];
+  uint32_t q[NT][D / 16][2], coming[NT][D / 16][2];
+  float o[NT][D / 16][4];
+  float m[NT][2], l[NT][2];
 
   __device__ __forceinline__ static int swizzle(int row, int chunk) { return chunk ^ (row & 7); }
-  __device__ __forceinline__ void start(const T* qp, long long stride, int rows, int lane) {
-    const int r0 = lane >> 2, c0 = (lane & 3) * 2;
+  // query rows of the work behind the present one, on their way while that is worked on
+  __device__ __forceinline__ void prefetch(const T* qp, long long stride, int rows, int lane) {
 #pragma unroll
-    for (int k = 0; k < D / 16; ++k)
+    for (int t = 0; t < NT; ++t)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int r = r0 + (i & 1) * 8, c = k * 16 + c0 + (i >> 1) * 8;
-        q[k][i] = r < rows ? *reinterpret_cast<const uint32_t*>(qp + r * stride + c) : 0u;
+      for (int k = 0; k < D / 16; ++k)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const int r = t * 8 + (lane >> 2), c = k * 16 + (lane & 3) * 2 + i * 8;
+          coming[t][k][i] = r < rows ? *reinterpret_cast<const uint32_t*>(qp + r * stride + c) : 0u;
+        }
+  }
+  __device__ __forceinline__ void start(int) {
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+#pragma unroll
+      for (int k = 0; k < D / 16; ++k) {
+        q[t][k][0] = coming[t][k][0];
+        q[t][k][1] = coming[t][k][1];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[t][k][i] = 0.f;
       }
 #pragma unroll
-    for (int n = 0; n < D / 8; ++n)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) o[n][i] = 0.f;
-    m[0] = m[1] = -INFINITY;
-    l[0] = l[1] = 0.f;
+      for (int i = 0; i < 2; ++i) { m[t][i] = -INFINITY; l[t][i] = 0.f; }
+    }
   }
-  // keys j0 .. j0 + 15 of the sequence, in shared memory at ks and vs
-  __device__ __forceinline__ void step(uint32_t ks, uint32_t vs, int j0, const Span& span, float scale, int lane) {
-    float s[2][4] = {};
+  // keys j0 .. j0 + 15 of the sequence, in shared memory at `keys` and `values`
+  __device__ __forceinline__ void step(const unsigned char* keys, const unsigned char* values, int j0, const Span& span, float scale, int lane) {
+    const uint32_t ks = smem_u32(keys), vs = smem_u32(values);
+    float s[NT][4] = {};
 #pragma unroll
     for (int k = 0; k < D / 16; ++k) {
-      uint32_t b[4];
-      const int row = (lane & 7) + ((lane >> 4) << 3), chunk = 2 * k + ((lane >> 3) & 1);
-      ldmatrix4(ks + row * ROW_BYTES + swizzle(row, chunk) * 16, b);
-      mma16816(s[0], q[k], b[0], b[1]);
-      mma16816(s[1], q[k], b[2], b[3]);
+      uint32_t a[4];
+      const int row = lane & 15, chunk = 2 * k + (lane >> 4);
+      ldmatrix4(ks + row * ROW_BYTES + swizzle(row, chunk) * 16, a);
+#pragma unroll
+      for (int t = 0; t < NT; ++t) mma16816(s[t], a, q[t][k][0], q[t][k][1]);
     }
     const bool whole = j0 >= span.lo ? j0 + KEYS <= span.n : j0 + KEYS <= span.sink_end;
+    if (!whole) {
+      const bool first = span.sees(j0 + (lane >> 2)), second = span.sees(j0 + (lane >> 2) + 8);
 #pragma unroll
-    for (int t = 0; t < 2; ++t)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        s[t][i] *= scale;
-        if (!whole && !span.sees(j0 + t * 8 + (lane & 3) * 2 + (i & 1))) s[t][i] = -INFINITY;
-      }
-    float top[2];
-#pragma unroll
-    for (int r = 0; r < 2; ++r)
-      top[r] = max_of_keys(fmaxf(fmaxf(s[0][2 * r], s[0][2 * r + 1]), fmaxf(s[1][2 * r], s[1][2 * r + 1])));
-    if (__any_sync(0xffffffffu, top[0] > m[0] || top[1] > m[1])) {
-#pragma unroll
-      for (int r = 0; r < 2; ++r) {
-        const float up = fmaxf(m[r], top[r]);
-        const float by = m[r] == -INFINITY ? 0.f : ex2_approx(m[r] - up);
-        l[r] *= by;
-        m[r] = up;
-#pragma unroll
-        for (int n = 0; n < D / 8; ++n) { o[n][2 * r] *= by; o[n][2 * r + 1] *= by; }
+      for (int t = 0; t < NT; ++t) {
+        if (!first) s[t][0] = s[t][1] = -INFINITY;
+        if (!second) s[t][2] = s[t][3] = -INFINITY;
       }
     }
-    // Probabilities in two bf16 parts, the upper bits and the rest: the products have time to spare, and the result the accuracy of
-    // fp32.  The rest is kept above zero, so that an infinite value stays one (of a weight that is 1 at least 1e-30 is nothing).
-    uint32_t hi[4], lo[4];
+    uint32_t hi[NT][2], lo[NT][2];
 #pragma unroll
-    for (int t = 0; t < 2; ++t)
+    for (int t = 0; t < NT; ++t) {
+      float top[2];
 #pragma unroll
-      for (int r = 0; r < 2; ++r) {
-        const float ref = m[r] == -INFINITY ? 0.f : m[r];
-        const float p0 = ex2_approx(s[t][2 * r] - ref), p1 = ex2_approx(s[t][2 * r + 1] - ref);
-        l[r] += p0 + p1;
+      for (int i = 0; i < 2; ++i) {
+        top[i] = fmaxf(s[t][i], s[t][2 + i]);
+#pragma unroll
+        for (int x = 4; x < 32; x <<= 1) top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], x));
+        top[i] *= scale;
+      }
+      if (__any_sync(0xffffffffu, top[0] > m[t][0] || top[1] > m[t][1])) {
+        float by[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const float up = fmaxf(m[t][i], top[i]);
+          by[i] = m[t][i] == -INFINITY ? 0.f : ex2_approx(m[t][i] - up);
+          l[t][i] *= by[i];
+          m[t][i] = up;
+        }
+#pragma unroll
+        for (int n = 0; n < D / 16; ++n)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) o[t][n][i] *= by[i & 1];
+      }
+      // Probabilities in two bf16 parts, the upper bits and the rest: the products have time to spare, and the result the accuracy of
+      // fp32.  The rest is kept above zero, so that an infinite value stays one (of a weight that is 1 at least 1e-30 is nothing).
+      const float ref0 = m[t][0] == -INFINITY ? 0.f : -m[t][0], ref1 = m[t][1] == -INFINITY ? 0.f : -m[t][1];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const float p0 = ex2_approx(fmaf(s[t][2 * h], scale, ref0)), p1 = ex2_approx(fmaf(s[t][2 * h + 1], scale, ref1));
+        l[t][0] += p0;
+        l[t][1] += p1;
         const uint32_t u0 = __float_as_uint(p0) & 0xffff0000u, u1 = __float_as_uint(p1) & 0xffff0000u;
-        hi[2 * t + r] = __byte_perm(u0, u1, 0x7632);
-        lo[2 * t + r] = pack_bf16x2(fmaxf(p0 - __uint_as_float(u0), 1e-30f), fmaxf(p1 - __uint_as_float(u1), 1e-30f));
+        hi[t][h] = transpose8x8(__byte_perm(u0, u1, 0x7632));
+        lo[t][h] = transpose8x8(pack_bf16x2(fmaxf(p0 - __uint_as_float(u0), 1e-30f), fmaxf(p1 - __uint_as_float(u1), 1e-30f)));
       }
+    }
 #pragma unroll
-    for (int n = 0; n < D / 8; n += 2) {
-      uint32_t b[4];
-      const int row = lane & 15, chunk = n + (lane >> 4);
-      ldmatrix4t(vs + row * ROW_BYTES + swizzle(row, chunk) * 16, b);
-      mma16816(o[n], hi, b[0], b[1]);
-      mma16816(o[n], lo, b[0], b[1]);
-      mma16816(o[n + 1], hi, b[2], b[3]);
-      mma16816(o[n + 1], lo, b[2], b[3]);
+    for (int n = 0; n < D / 16; ++n) {
+      uint32_t a[4];
+      const int row = (lane & 7) + ((lane >> 4) << 3), chunk = 2 * n + ((lane >> 3) & 1);
+      ldmatrix4t(vs + row * ROW_BYTES + swizzle(row, chunk) * 16, a);
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        mma16816(o[t][n], a, hi[t][0], hi[t][1]);
+        mma16816(o[t][n], a, lo[t][0], lo[t][1]);
+      }
     }
   }
-  __device__ __forceinline__ void finish(int) {
-    l[0] = sum_of_keys(l[0]);
-    l[1] = sum_of_keys(l[1]);
-  }
-  // rows of the result in fp32: [rows][D] and {m, l} behind them
-  __device__ __forceinline__ void put(float* buf, float* ml, int rows, int lane) const {
-    const int r0 = lane >> 2, c0 = (lane & 3) * 2;
+  // the result in fp32: [rows][D] by place(), and {m, l} of each row
+  __device__ __forceinline__ void put(float* buf, float* ml, int rows, int lane) {
 #pragma unroll
-    for (int r = 0; r < 2; ++r) {
-      const int row = r0 + 8 * r;
-      if (row >= rows) continue;
+    for (int t = 0; t < NT; ++t)
 #pragma unroll
-      for (int n = 0; n < D / 8; ++n) *reinterpret_cast<float2*>(buf + row * D + n * 8 + c0) = make_float2(o[n][2 * r], o[n][2 * r + 1]);
-      if ((lane & 3) == 0) { ml[2 * row] = m[r]; ml[2 * row + 1] = l[r]; }
-    }
+      for (int i = 0; i < 2; ++i) {
+#pragma unroll
+        for (int x = 4; x < 32; x <<= 1) l[t][i] += __shfl_xor_sync(0xffffffffu, l[t][i], x);
+        const int row = t * 8 + (lane & 3) * 2 + i;
+        if (row >= rows) continue;
+#pragma unroll
+        for (int n = 0; n < D / 16; ++n) {
+          const int col = n * 16 + (lane >> 2);
+          buf[row * D + place(row, col)] = o[t][n][i];
+          buf[row * D + place(row, col + 8)] = o[t][n][2 + i];
+        }
+        if (lane < 4) { ml[2 * row] = m[t][i]; ml[2 * row + 1] = l[t][i]; }
+      }
   }
+  // where column `col` of a row lies: the lanes that write at a time are four rows apart, in different banks
+  __device__ __forceinline__ static int place(int row, int col) { return col ^ (((row >> 1) & 3) << 3); }
 };
 
-// fp32 storage: the same on the CUDA cores.  Scores: four lanes to a key, which divide d; values: a lane holds
-// four columns (at d = 64 half a warp each takes every other key).  ROWS query rows are worked on.
+// fp32 storage: the same on the CUDA cores, two multiply-adds to an instruction.  Scores: four lanes to a key, which divide d; values: a
+// lane holds four columns (at d = 64 half a warp each takes every other key).  R query rows are worked on.
 template <int D, int R>
 struct WarpFma {
   using T = float;
-  static constexpr int ROWS = R, KEYS = 8;
+  static constexpr int ROWS = R, KEYS = 8, STAGES = 3;
   static constexpr int ROW_BYTES = D * 4, CHUNKS = ROW_BYTES / 16;
   static constexpr int SPLIT = 128 / D;      // keys that are worked on side by side in P V
-  float o[R][4];
+  static constexpr bool HELD = R * D <= 256; // query rows in registers (a quarter of each: R D / 4), otherwise in shared memory
+  static constexpr int SCRATCH = HELD ? KEYS * R : R * D + KEYS * R;
+  f32x2 o[R][2];
   float m[R], l[R];
-  const float* qs;                           // [R][D] in shared memory, the warp's own copy
-  float* ps;                                 // [KEYS][R] probabilities
+  float4 held[HELD ? R : 1][CHUNKS / 4];
+  float coming[R * D / 32];
+  float *qs, *ps;                            // the warp's own: [R][D] query rows, [KEYS][R] probabilities
 
   // eight lanes that read at a time are two keys by four chunks: chunks of neighbouring keys in different banks
   __device__ __forceinline__ static int swizzle(int row, int chunk) { return chunk ^ (((row & 1) << 2) | ((row >> 1) & 3)); }
-  __device__ __forceinline__ void start(const T* qp, long long stride, int rows, int lane, float* scratch) {
-    qs = scratch;
-    ps = scratch + R * D;
+  __device__ __forceinline__ void prefetch(const T* qp, long long stride, int rows, int lane) {
+#pragma unroll
+    for (int i = 0; i < R * D / 32; ++i) {
+      const int e = i * 32 + lane;
+      coming[i] = e / D < rows ? qp[e / D * stride + e % D] : 0.f;
+    }
+  }
+  __device__ __forceinline__ void start(int lane, float* scratch, float* buf) {
+    ps = scratch;
+    qs = HELD ? buf : scratch + KEYS * R;    // (held rows only pass through the hand-over buffer)
     __syncwarp();
-    for (int i = lane; i < R * D; i += 32) scratch[i] = i / D < rows ? qp[(i / D) * stride + i % D] : 0.f;
+#pragma unroll
+    for (int i = 0; i < R * D / 32; ++i) qs[i * 32 + lane] = coming[i];
     __syncwarp();
+    if (HELD) {
+#pragma unroll
+      for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int i = 0; i < CHUNKS / 4; ++i) held[r][i] = *reinterpret_cast<const float4*>(qs + r * D + ((lane & 3) + 4 * i) * 4);
+    }
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) o[r][i] = 0.f;
+      o[r][0] = o[r][1] = pack2(0.f, 0.f);
       m[r] = -INFINITY;
       l[r] = 0.f;
     }
   }
   __device__ __forceinline__ void step(const unsigned char* ks, const unsigned char* vs, int j0, const Span& span, float scale, int lane) {
     const int key = lane >> 2, quarter = lane & 3;
-    float s[R];
+    f32x2 s2[R][2];
 #pragma unroll
-    for (int r = 0; r < R; ++r) s[r] = 0.f;
+    for (int r = 0; r < R; ++r) s2[r][0] = s2[r][1] = pack2(0.f, 0.f);
 #pragma unroll
     for (int i = 0; i < CHUNKS / 4; ++i) {
       const int chunk = quarter + 4 * i;
       const float4 k = *reinterpret_cast<const float4*>(ks + key * ROW_BYTES + swizzle(key, chunk) * 16);
 #pragma unroll
       for (int r = 0; r < R; ++r) {
-        const float4 q = *reinterpret_cast<const float4*>(qs + r * D + chunk * 4);
-        s[r] = fmaf(q.x, k.x, fmaf(q.y, k.y, fmaf(q.z, k.z, fmaf(q.w, k.w, s[r]))));
+        const float4 q = HELD ? held[HELD ? r : 0][i] : *reinterpret_cast<const float4*>(qs + r * D + chunk * 4);
+        s2[r][0] = fma2(pack2(q.x, q.y), pack2(k.x, k.y), s2[r][0]);
+        s2[r][1] = fma2(pack2(q.z, q.w), pack2(k.z, k.w), s2[r][1]);
       }
     }
     const bool seen = span.sees(j0 + key);
-    float p[R];
+    float s[R], p[R];
+    bool up = false;
 #pragma unroll
     for (int r = 0; r < R; ++r) {
+      float a, b, c, d;
+      unpack2(s2[r][0], a, b);
+      unpack2(s2[r][1], c, d);
+      s[r] = (a + b) + (c + d);
       s[r] += __shfl_xor_sync(0xffffffffu, s[r], 1);
       s[r] += __shfl_xor_sync(0xffffffffu, s[r], 2);
       s[r] = seen ? s[r] * scale : -INFINITY;
-      float top = s[r];
+      up = up || s[r] > m[r];
+    }
+    if (__any_sync(0xffffffffu, up)) {       // a new maximum of some row
 #pragma unroll
-      for (int x = 4; x < 32; x <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
-      if (top > m[r]) {
+      for (int r = 0; r < R; ++r) {
+        float top = fmaxf(m[r], s[r]);
+#pragma unroll
+        for (int x = 4; x < 32; x <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
         const float by = m[r] == -INFINITY ? 0.f : ex2_approx(m[r] - top);
         m[r] = top;
         l[r] *= by;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) o[r][i] *= by;
+        o[r][0] = mul2(o[r][0], pack2(by, by));
+        o[r][1] = mul2(o[r][1], pack2(by, by));
       }
+    }
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
       p[r] = ex2_approx(s[r] - (m[r] == -INFINITY ? 0.f : m[r]));
       if (quarter == 0) l[r] += p[r];
     }
-    __syncwarp();
     if (quarter == 0) {
 #pragma unroll
       for (int r = 0; r < R; ++r) ps[key * R + r] = p[r];
@@ -310,56 +370,105 @@ struct WarpFma {
 #pragma unroll
       for (int r = 0; r < R; ++r) {
         const float w = ps[row * R + r];
-        o[r][0] = fmaf(w, v.x, o[r][0]);
-        o[r][1] = fmaf(w, v.y, o[r][1]);
-        o[r][2] = fmaf(w, v.z, o[r][2]);
-        o[r][3] = fmaf(w, v.w, o[r][3]);
+        o[r][0] = fma2(pack2(w, w), pack2(v.x, v.y), o[r][0]);
+        o[r][1] = fma2(pack2(w, w), pack2(v.z, v.w), o[r][1]);
       }
     }
+    __syncwarp();                            // the probabilities have been read
   }
-  __device__ __forceinline__ void finish(int) {
+  __device__ __forceinline__ void put(float* buf, float* ml, int rows, int lane) {
 #pragma unroll
     for (int r = 0; r < R; ++r) {
 #pragma unroll
       for (int x = 4; x < 32; x <<= 1) l[r] += __shfl_xor_sync(0xffffffffu, l[r], x);
-      l[r] = __shfl_sync(0xffffffffu, l[r], 0);
+      float v[4];
+      unpack2(o[r][0], v[0], v[1]);
+      unpack2(o[r][1], v[2], v[3]);
       if (SPLIT == 2) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) o[r][i] += __shfl_xor_sync(0xffffffffu, o[r][i], 16);
+        for (int i = 0; i < 4; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], 16);
       }
-    }
-  }
-  __device__ __forceinline__ void put(float* buf, float* ml, int rows, int lane) const {
-#pragma unroll
-    for (int r = 0; r < R; ++r) {
-      if (r >= rows) break;
-      if (lane < CHUNKS) *reinterpret_cast<float4*>(buf + r * D + lane * 4) = make_float4(o[r][0], o[r][1], o[r][2], o[r][3]);
+      if (r >= rows) continue;
+      if (lane < CHUNKS) *reinterpret_cast<float4*>(buf + r * D + lane * 4) = make_float4(v[0], v[1], v[2], v[3]);
       if (lane == 0) { ml[2 * r] = m[r]; ml[2 * r + 1] = l[r]; }
     }
   }
+  __device__ __forceinline__ static int place(int, int col) { return col; }
 };
+
+template <typename W>
+constexpr int scratch_floats() {
+  if constexpr (std::is_same<typename W::T, float>::value) return W::SCRATCH;
+  else return 0;
+}
 
 template <typename W, int D>
 struct PagedCfg {
   static constexpr bool MMA = std::is_same<typename W::T, __nv_bfloat16>::value;
   static constexpr int U = kPagedWarps * W::KEYS;                  // rows of a unit
   static constexpr int STEP_BYTES = 2 * W::KEYS * W::ROW_BYTES;    // keys and values of a warp's step
-  static constexpr int STAGES = 3;
+  static constexpr int STAGES = W::STAGES;
   static constexpr int RING = STAGES * STEP_BYTES;
-  static constexpr int SCRATCH = MMA ? 0 : (W::ROWS * D + W::KEYS * W::ROWS) * 4;
+  static constexpr int SCRATCH = scratch_floats<W>() * 4;
   static constexpr int OFF_SCRATCH = kPagedWarps * RING;
-  static constexpr int OFF_FLAG = OFF_SCRATCH + kPagedWarps * SCRATCH;
-  static constexpr int OFF_ML = OFF_FLAG + 16;                              // [kPagedWarps][ROWS]{m, l}
+  static constexpr int OFF_ML = OFF_SCRATCH + kPagedWarps * SCRATCH;        // [kPagedWarps][ROWS]{m, l}
   static constexpr int OFF_JOIN = OFF_ML + kPagedWarps * W::ROWS * 8;       // [kPagedWarps][rows][D], as many rows as there are
-  static_assert(OFF_JOIN % 16 == 0, "alignment");
-  static int smem(int rows) { return OFF_JOIN + kPagedWarps * rows * D * 4; }
+  static_assert(OFF_JOIN % 16 == 0 && SCRATCH % 16 == 0, "alignment");
+  // rows of a hand-over buffer: as many as there are (query rows in fp32 pass through it in whole tiles)
+  __host__ __device__ static int buffer_rows(int group) { return MMA && group < W::ROWS ? group : W::ROWS; }
+  static int smem(int group) {
+    return OFF_JOIN + kPagedWarps * buffer_rows(group) * D * 4;
+  }
 };
 
-// Where a CTA or one of its warps stands on the line of units.
+__device__ __forceinline__ void add_scaled(float4& o, float4 v, float by) {
+  o.x = fmaf(v.x, by, o.x);
+  o.y = fmaf(v.y, by, o.y);
+  o.z = fmaf(v.z, by, o.z);
+  o.w = fmaf(v.w, by, o.w);
+}
+
+// The line of units: of every (sequence, key head, row tile) kPairUnits and then its tiles.  Part c of `parts` is [total c / parts,
+// total (c + 1) / parts); the part that holds position x:
+__device__ __forceinline__ int part_of(long long x, long long parts, long long total) { return (int)(((x + 1) * parts + total - 1) / total) - 1; }
+
+// Where a CTA or one of its warps stands in its part: tiles [tile, last) of a (sequence, key head, row tile).
 struct Place {
-  int b, h, rt, tile;
-  long long left;                // units from here to the end of the part
+  int b, h, rt, tile, last;
+  long long pos, end;                        // where the next one begins on the line, where the part ends
+  __device__ __forceinline__ bool there() const { return tile < last; }
+  // tiles of the part in the one that begins at `base`, from position `from` on
+  __device__ __forceinline__ void cut(long long base, long long from, int tiles) {
+    const long long first = from - base - kPairUnits, behind = min(end, base + kPairUnits + tiles) - base - kPairUnits;
+    tile = (int)max(0LL, first);
+    last = (int)max(0LL, behind);
+    pos = base + kPairUnits + tiles;
+  }
+  // the next one; `span` follows the sequence
+  __device__ __forceinline__ void next(const PagedParams& prm, Span& span, int U) {
+    tile = last = 0;
+    while (!there() && pos < end) {
+      if (++rt == prm.row_tiles) {
+        rt = 0;
+        if (++h == prm.heads_kv) {
+          h = 0;
+          ++b;
+          span = Span(prm, b, U);
+        }
+      }
+      cut(pos, pos, span.tiles);
+    }
+  }
 };
+
+// four columns of the result; a row that sees nothing: zero, log-sum-exp -inf
+template <typename T>
+__device__ __forceinline__ void finish_row(const PagedParams& prm, int b, int head, int col, float4 o, float m, float l) {
+  if (l == 0.f) o = make_float4(0.f, 0.f, 0.f, 0.f);
+  else o = make_float4(o.x / l, o.y / l, o.z / l, o.w / l);
+  store4(static_cast<T*>(prm.o) + b * prm.o_b + head * prm.o_h + col, o);
+  if (col == 0 && prm.lse) prm.lse[(size_t)b * prm.heads_q + head] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
+}
 
 template <typename W, int D>
 __global__ void __launch_bounds__(kPagedThreads) paged_kernel(const __grid_constant__ PagedParams prm) {
@@ -370,12 +479,12 @@ __global__ void __launch_bounds__(kPagedThreads) paged_kernel(const __grid_const
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int per = prm.heads_kv * prm.row_tiles;              // (key head, row tile) pairs of a sequence
   const long long total = prm.units[prm.batch] * per;
-  const long long parts = min((long long)gridDim.x, total);  // every part has a unit at least
+  const long long parts = min((long long)gridDim.x, total);
   if (blockIdx.x >= parts) { let_next_start(); return; }
-  const long long begin = total * blockIdx.x / parts, end = total * (blockIdx.x + 1) / parts;
-
   Place at;
   {
+    const long long begin = total * blockIdx.x / parts;
+    at.end = total * (blockIdx.x + 1) / parts;
     int lo = 0, hi = prm.batch - 1;                          // last sequence whose units begin at or before `begin`
     while (lo < hi) {
       const int mid = (lo + hi + 1) >> 1;
@@ -383,64 +492,68 @@ __global__ void __launch_bounds__(kPagedThreads) paged_kernel(const __grid_const
       else hi = mid - 1;
     }
     const long long off = begin - prm.units[lo] * per;
-    const int tiles = (int)(prm.units[lo + 1] - prm.units[lo]);
-    const int pair = (int)(off / tiles);
+    const int each = (int)(prm.units[lo + 1] - prm.units[lo]);
+    const int pair = (int)(off / each);
     at.b = lo;
     at.h = pair / prm.row_tiles;
     at.rt = pair % prm.row_tiles;
-    at.tile = (int)(off % tiles);
-    at.left = end - begin;
+    at.cut(prm.units[lo] * per + (long long)pair * each, begin, each - kPairUnits);
   }
-  auto next_pair = [&](Place& p) {
-    p.tile = 0;
-    if (++p.rt == prm.row_tiles) {
-      p.rt = 0;
-      if (++p.h == prm.heads_kv) { p.h = 0; ++p.b; }
-    }
-  };
+  Span span(prm, at.b, C::U);
+  if (!at.there()) at.next(prm, span, C::U);
 
   unsigned char* ring = smem + warp * C::RING;
   const uint32_t s_ring = smem_u32(ring);
   // ---- copies: a unit's rows of this warp into the next stage; the page of a row is looked up a step ahead
   Place ld = at;
-  Span ld_span(prm, ld.b, C::U);
+  Span ld_span = span;
   int ld_stage = 0;
+  constexpr int CH = W::CHUNKS, RPI = 32 / CH;               // 16-byte chunks of a row, rows of an instruction
+  const bool aligned = prm.page_rows % W::KEYS == 0;         // a step's rows are in one page, side by side
+  const long long page_elements = (long long)prm.heads_kv * prm.page_rows * D;
   int page = 0;
   bool seen = false;
-  constexpr int CH = W::CHUNKS, RPI = 32 / CH;               // 16-byte chunks of a row, rows of an instruction
   auto look_up = [&]() {                                     // page of row `lane` of the coming step
     seen = false;
-    if (ld.left > 0 && lane < W::KEYS) {
+    if (ld.there() && lane < W::KEYS) {
       const int j = ld_span.tile(ld.tile) * C::U + warp * W::KEYS + lane;
       seen = ld_span.sees(j);
       if (seen) page = prm.page_table[(size_t)ld.b * prm.pages_per_sequence + j / prm.page_rows];
     }
   };
   auto load = [&]() {
-    if (ld.left > 0) {
-      const uint32_t dst = s_ring + ld_stage * C::STEP_BYTES + lane / CH * W::ROW_BYTES;
+    if (ld.there()) {
+      const int row0 = lane / CH, c = lane % CH;
+      const int j = ld_span.tile(ld.tile) * C::U + warp * W::KEYS;
+      const uint32_t dst = s_ring + ld_stage * C::STEP_BYTES + row0 * W::ROW_BYTES;
       int id = seen ? page : -1;
       if (seen && (unsigned)page >= (unsigned)prm.pages) {   // not a page: flagged, its rows read as zeros
         atomicCAS(prm.status, 0, CA_ERR_BAD_INDEX);
         id = -1;
       }
-      const int j = ld_span.tile(ld.tile) * C::U + warp * W::KEYS + lane;
-      const int slot = ld.h * prm.page_rows + j % prm.page_rows;
-      const long long page_elements = (long long)prm.heads_kv * prm.page_rows * D;
+      if (aligned && __all_sync(0xffffffffu, id >= 0 || lane >= W::KEYS)) {
+        const long long off = __shfl_sync(0xffffffffu, id, 0) * page_elements + (long long)(ld.h * prm.page_rows + j % prm.page_rows + row0) * D + c * (16 / (int)sizeof(T));
+        const T* k = static_cast<const T*>(prm.k_pages) + off;
+        const T* v = static_cast<const T*>(prm.v_pages) + off;
 #pragma unroll
-      for (int i = 0; i < W::KEYS / RPI; ++i) {
-        const int row = i * RPI + lane / CH, c = lane % CH;
-        const int row_id = __shfl_sync(0xffffffffu, id, row), row_slot = __shfl_sync(0xffffffffu, slot, row);
-        const long long off = row_id >= 0 ? row_id * page_elements + (long long)row_slot * D + c * (16 / (int)sizeof(T)) : 0;
-        const uint32_t to = dst + i * RPI * W::ROW_BYTES + W::swizzle(row, c) * 16;
-        cp_async16(to, static_cast<const T*>(prm.k_pages) + off, row_id >= 0);
-        cp_async16(to + W::KEYS * W::ROW_BYTES, static_cast<const T*>(prm.v_pages) + off, row_id >= 0);
+        for (int i = 0; i < W::KEYS / RPI; ++i) {
+          const uint32_t to = dst + i * RPI * W::ROW_BYTES + W::swizzle(i * RPI + row0, c) * 16;
+          cp_async16(to, k + i * RPI * D, true);
+          cp_async16(to + W::KEYS * W::ROW_BYTES, v + i * RPI * D, true);
+        }
+      } else {
+        const int slot = ld.h * prm.page_rows + (j + lane) % prm.page_rows;
+#pragma unroll
+        for (int i = 0; i < W::KEYS / RPI; ++i) {
+          const int row = i * RPI + row0;
+          const int row_id = __shfl_sync(0xffffffffu, id, row), row_slot = __shfl_sync(0xffffffffu, slot, row);
+          const long long off = row_id >= 0 ? row_id * page_elements + (long long)row_slot * D + c * (16 / (int)sizeof(T)) : 0;
+          const uint32_t to = dst + i * RPI * W::ROW_BYTES + W::swizzle(row, c) * 16;
+          cp_async16(to, static_cast<const T*>(prm.k_pages) + off, row_id >= 0);
+          cp_async16(to + W::KEYS * W::ROW_BYTES, static_cast<const T*>(prm.v_pages) + off, row_id >= 0);
+        }
       }
-      if (--ld.left > 0 && ++ld.tile == ld_span.tiles) {
-        const int b = ld.b;
-        next_pair(ld);
-        if (ld.b != b) ld_span = Span(prm, ld.b, C::U);
-      }
+      if (++ld.tile == ld.last) ld.next(prm, ld_span, C::U);
     }
     cp_async_commit();
     ld_stage = ld_stage + 1 == C::STAGES ? 0 : ld_stage + 1;
@@ -450,112 +563,154 @@ __global__ void __launch_bounds__(kPagedThreads) paged_kernel(const __grid_const
 #pragma unroll
   for (int i = 0; i < C::STAGES - 1; ++i) load();
 
-  // an element of the result; a row that sees nothing: zero, log-sum-exp -inf
-  auto finish_row = [&](int b, int head, int col, float o, float m, float l) {
-    static_cast<T*>(prm.o)[b * prm.o_b + head * prm.o_h + col] = from_f32<T>(l == 0.f ? 0.f : o / l);
-    if (col == 0 && prm.lse) prm.lse[(size_t)b * prm.heads_q + head] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
-  };
   W w;
   int stage = 0;
   float* join = reinterpret_cast<float*>(smem + C::OFF_JOIN);
   float* ml = reinterpret_cast<float*>(smem + C::OFF_ML);
-  volatile int* flag = reinterpret_cast<volatile int*>(smem + C::OFF_FLAG);
-  while (at.left > 0) {
+  auto head_of = [&](const Place& p) { return p.h * prm.group + p.rt * W::ROWS; };        // query head of row 0
+  auto rows_of = [&](const Place& p) { return min(prm.group - p.rt * W::ROWS, W::ROWS); };
+  auto prefetch_queries = [&](const Place& p) {
+    w.prefetch(static_cast<const T*>(prm.q) + p.b * prm.q_b + head_of(p) * prm.q_h, prm.q_h, rows_of(p), lane);
+  };
+  if (at.there()) prefetch_queries(at);
+  const int all_rows = C::buffer_rows(prm.group);
+  float* mine = join + warp * all_rows * D;
+  while (at.there()) {
     // ---- one (sequence, key head, row tile): its units in this CTA's part
-    const Span span(prm, at.b, C::U);
-    const int rows = min(prm.group - at.rt * W::ROWS, W::ROWS);
-    const int head0 = at.h * prm.group + at.rt * W::ROWS;    // query head of row 0
-    const T* qp = static_cast<const T*>(prm.q) + at.b * prm.q_b + head0 * prm.q_h;
-    if constexpr (C::MMA) w.start(qp, prm.q_h, rows, lane);
-    else w.start(qp, prm.q_h, rows, lane, reinterpret_cast<float*>(smem + C::OFF_SCRATCH + warp * C::SCRATCH));
-    const int first_tile = at.tile;
-    const int last_tile = (int)min((long long)span.tiles, first_tile + at.left);      // behind the last
+    const int rows = rows_of(at), head0 = head_of(at);
+    if constexpr (C::MMA) w.start(lane);
+    else w.start(lane, reinterpret_cast<float*>(smem + C::OFF_SCRATCH + warp * C::SCRATCH), mine);
+    const int first_tile = at.tile, last_tile = at.last;
+    Place coming = at;
+    Span coming_span = span;
+    coming.next(prm, coming_span, C::U);
+    if (coming.there()) prefetch_queries(coming);
 #pragma unroll 1
     for (int t = first_tile; t < last_tile; ++t) {
       cp_async_wait<C::STAGES - 2>();
       __syncwarp();
       const int j0 = span.tile(t) * C::U + warp * W::KEYS;
-      const int off = stage * C::STEP_BYTES;
+      const unsigned char* keys = ring + stage * C::STEP_BYTES;
       load();                                                // into the stage that the step before has read
-      if (j0 < span.n) {
-        if constexpr (C::MMA) w.step(s_ring + off, s_ring + off + W::KEYS * W::ROW_BYTES, j0, span, prm.scale_log2, lane);
-        else w.step(ring + off, ring + off + W::KEYS * W::ROW_BYTES, j0, span, prm.scale_log2, lane);
-      }
+      if (j0 < span.n) w.step(keys, keys + W::KEYS * W::ROW_BYTES, j0, span, prm.scale_log2, lane);
       __syncwarp();
       stage = stage + 1 == C::STAGES ? 0 : stage + 1;
     }
-    at.left -= last_tile - first_tile;
-    w.finish(lane);
     // ---- the warps' results into one
     const bool whole = first_tile == 0 && last_tile == span.tiles;
-    const int all_rows = min(prm.group, W::ROWS);            // rows of a hand-over buffer
-    __syncthreads();                                         // the buffers have been read
-    w.put(join + warp * all_rows * D, ml + warp * 2 * W::ROWS, rows, lane);
+    w.put(mine, ml + warp * 2 * W::ROWS, rows, lane);
     __syncthreads();
-    float* part = prm.partial + (size_t)(2 * blockIdx.x + (first_tile == 0 ? 1 : 0)) * W::ROWS * (D + 2);
-    for (int i = threadIdx.x; i < rows * D; i += kPagedThreads) {
-      const int r = i / D;
-      float top = -INFINITY, o = 0.f, l = 0.f;
+    float* part = prm.partial + (size_t)(2 * blockIdx.x + (first_tile == 0 ? 1 : 0)) * W::ROWS * (D + 4);
+    for (int i = threadIdx.x; i < rows * (D / 4); i += kPagedThreads) {
+      const int r = i / (D / 4), col = i % (D / 4) * 4;
+      float top = -INFINITY, l = 0.f;
+      float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
       for (int x = 0; x < kPagedWarps; ++x) top = fmaxf(top, ml[(x * W::ROWS + r) * 2]);
 #pragma unroll
       for (int x = 0; x < kPagedWarps; ++x) {
         const float m = ml[(x * W::ROWS + r) * 2], by = m == -INFINITY ? 0.f : ex2_approx(m - top);
-        o = fmaf(join[x * all_rows * D + i], by, o);
+        const float4 v = *reinterpret_cast<const float4*>(join + (x * all_rows + r) * D + W::place(r, col));
+        add_scaled(o, v, by);
         l = fmaf(ml[(x * W::ROWS + r) * 2 + 1], by, l);
       }
       if (whole) {
-        finish_row(at.b, head0 + r, i % D, o, top, l);
+        finish_row<T>(prm, at.b, head0 + r, col, o, top, l);
       } else {
-        part[i] = o;
-        if (i % D == 0) { part[W::ROWS * D + 2 * r] = top; part[W::ROWS * D + 2 * r + 1] = l; }
+        *reinterpret_cast<float4*>(part + r * D + col) = o;
+        if (col == 0) *reinterpret_cast<float2*>(part + W::ROWS * D + 2 * r) = make_float2(top, l);
       }
     }
-    if (!whole) {
-      // ---- the last of the CTAs that share these rows joins their results, in the order of the rows
-      const long long base = prm.units[at.b] * per + (long long)(at.h * prm.row_tiles + at.rt) * span.tiles;
-      const int cta0 = (int)(((base + 1) * parts + total - 1) / total) - 1;
-      const int cta1 = (int)(((base + span.tiles) * parts + total - 1) / total) - 1;
-      __threadfence();
-      __syncthreads();
-      if (threadIdx.x == 0) *flag = atomicAdd(&prm.arrived[((long long)at.b * prm.heads_kv + at.h) * prm.row_tiles + at.rt], 1) == cta1 - cta0;
-      __syncthreads();
-      if (*flag) {
-        __threadfence();
-        for (int i = threadIdx.x; i < rows * D; i += kPagedThreads) {
-          const int r = i / D;
-          float top = -INFINITY, o = 0.f, l = 0.f;
-          for (int c = cta0; c <= cta1; ++c) {
-            const float* p = prm.partial + (size_t)(2 * c + (c == cta0 ? 1 : 0)) * W::ROWS * (D + 2);
-            const float pm = __ldcg(p + W::ROWS * D + 2 * r), pl = __ldcg(p + W::ROWS * D + 2 * r + 1), po = __ldcg(p + i);
-            const float up = fmaxf(top, pm);
-            const float w0 = top == -INFINITY ? 0.f : ex2_approx(top - up), w1 = pm == -INFINITY ? 0.f : ex2_approx(pm - up);
-            o = o * w0 + po * w1;
-            l = l * w0 + pl * w1;
-            top = up;
-          }
-          finish_row(at.b, head0 + r, i % D, o, top, l);
-        }
-      }
-    }
-    next_pair(at);
+    __syncthreads();                                         // the hand-over buffers have been read
+    at = coming;
+    span = coming_span;
   }
   let_next_start();
   cp_async_wait<0>();
 }
 
+// Results of the parts that share a (sequence, key head, row tile) into one, in the order of the rows, whichever was
+// finished first.  A CTA takes two query rows: 256 threads are a float4 of a row each, by groups of parts (part g, g + groups, ...), and
+// have the loads of eight parts in flight; then the groups are joined in shared memory.
+constexpr int kJoinThreads = 256, kJoinRows = 2;
+template <typename W, int D>
+__global__ void __launch_bounds__(kJoinThreads) paged_join_kernel(const __grid_constant__ PagedParams prm, int ctas) {
+  using C = PagedCfg<W, D>;
+  wait_for_previous();
+  let_next_start();
+  const int chunks = ceil_div_device(min(prm.group, W::ROWS), kJoinRows);
+  const int chunk = blockIdx.x % chunks, pair = blockIdx.x / chunks, per = prm.heads_kv * prm.row_tiles;
+  const int b = pair / per, h = pair % per / prm.row_tiles, rt = pair % prm.row_tiles;
+  const long long total = prm.units[prm.batch] * per, parts = min((long long)ctas, total);
+  const int each = (int)(prm.units[b + 1] - prm.units[b]);
+  const long long base = prm.units[b] * per + (long long)(pair % per) * each;
+  const int cta0 = part_of(base + kPairUnits, parts, total), cta1 = part_of(base + each - 1, parts, total);
+  const int row0 = chunk * kJoinRows, rows = min(min(prm.group - rt * W::ROWS, W::ROWS) - row0, kJoinRows);
+  if (cta0 == cta1 || rows <= 0) return;
+  constexpr int ITEMS = kJoinRows * D / 4, GROUPS = kJoinThreads / ITEMS;
+  __shared__ float4 sum[GROUPS][ITEMS];
+  __shared__ float2 ml[GROUPS][ITEMS];
+  const int item = threadIdx.x % ITEMS, g = threadIdx.x / ITEMS, r = min(item / (D / 4), rows - 1), col = item % (D / 4) * 4;
+  float top = -INFINITY, l = 0.f;
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 1
+  for (int c = cta0 + g; c <= cta1; c += 8 * GROUPS) {
+    float2 pml[8];
+    float4 po[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const int cc = c + k * GROUPS;
+      pml[k] = make_float2(-INFINITY, 0.f);
+      po[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (cc <= cta1) {
+        const float* p = prm.partial + (size_t)(2 * cc + (cc == cta0 ? 1 : 0)) * W::ROWS * (D + 4);
+        pml[k] = *reinterpret_cast<const float2*>(p + W::ROWS * D + 2 * (row0 + r));
+        po[k] = *reinterpret_cast<const float4*>(p + (row0 + r) * D + col);
+      }
+    }
+    float up = top;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) up = fmaxf(up, pml[k].x);
+    const float by = top == -INFINITY ? 0.f : ex2_approx(top - up);
+    o.x *= by; o.y *= by; o.z *= by; o.w *= by;
+    l *= by;
+    top = up;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const float wk = pml[k].x == -INFINITY ? 0.f : ex2_approx(pml[k].x - top);
+      add_scaled(o, po[k], wk);
+      l = fmaf(pml[k].y, wk, l);
+    }
+  }
+  sum[g][item] = o;
+  ml[g][item] = make_float2(top, l);
+  __syncthreads();
+  if (g > 0 || item / (D / 4) >= rows) return;
+#pragma unroll
+  for (int k = 1; k < GROUPS; ++k) top = fmaxf(top, ml[k][item].x);
+  const float own = ml[0][item].x == -INFINITY ? 0.f : ex2_approx(ml[0][item].x - top);
+  o.x *= own; o.y *= own; o.z *= own; o.w *= own;
+  l *= own;
+#pragma unroll
+  for (int k = 1; k < GROUPS; ++k) {
+    const float wk = ml[k][item].x == -INFINITY ? 0.f : ex2_approx(ml[k][item].x - top);
+    add_scaled(o, sum[k][item], wk);
+    l = fmaf(ml[k][item].y, wk, l);
+  }
+  finish_row<typename W::T>(prm, b, h * prm.group + rt * W::ROWS + row0 + r, col, o, top, l);
+}
+
 // ---- host side -------------------------------------------------------------------------------------------
 
 static int row_tile(const ca_cache_t& c) {
-  if (c.dtype == CA_DTYPE_BF16) return 16;
   const int group = c.heads_q / c.heads_kv;
+  if (c.dtype == CA_DTYPE_BF16) return group > 8 ? 16 : 8;
   return group >= 5 ? 8 : group >= 3 ? 4 : group;
 }
 
 struct PagedWs {
   int* status;
   long long* units;
-  int* arrived;
   float* partial;
   size_t bytes;
 };
@@ -565,8 +720,7 @@ static PagedWs carve_paged(const ca_cache_t& c, void* base) {
   const int rows = row_tile(c);
   w.status = k.take<int>(kStatusBytes / sizeof(int));
   w.units = k.take<long long>((size_t)c.batch + 1);
-  w.arrived = k.take<int>((size_t)c.batch * c.heads_kv * ceil_div(c.heads_q / c.heads_kv, rows));
-  w.partial = k.take<float>((size_t)2 * kPagedMaxCtas * rows * (c.head_dim + 2));
+  w.partial = k.take<float>((size_t)2 * kPagedMaxCtas * rows * (c.head_dim + 4));
   w.bytes = k.used();
   return w;
 }
@@ -579,13 +733,17 @@ static int launch_paged_d(PagedParams& prm, LaunchStream st) {
   CA_RETURN_IF_CUDA(cudaGetDevice(&dev));
   CA_RETURN_IF_CUDA(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
   prm.row_tiles = ceil_div(prm.group, W::ROWS);
-  const int smem = C::smem(min(prm.group, W::ROWS));
+  const int smem = C::smem(prm.group);
   auto kernel = paged_kernel<W, D>;
   CA_RETURN_IF_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
   launch_chained(paged_plan_kernel, 1, 1024, 0, st, prm, C::U);
   CA_LAUNCH_CHECK();
-  const int per_sm = min(3, (227 * 1024) / (smem + 1024));
-  launch_chained(kernel, min(kPagedMaxCtas, sms * per_sm), kPagedThreads, smem, st, prm);
+  const int per_sm = min(4, (228 * 1024) / (smem + 1024));
+  const int ctas = min(kPagedMaxCtas, sms * per_sm);
+  launch_chained(kernel, ctas, kPagedThreads, smem, st, prm);
+  CA_LAUNCH_CHECK();
+  const long long joins = (long long)prm.batch * prm.heads_kv * prm.row_tiles * ceil_div(min(prm.group, W::ROWS), kJoinRows);
+  launch_chained(paged_join_kernel<W, D>, (unsigned)joins, kJoinThreads, 0, st, prm, ctas);
   CA_LAUNCH_CHECK();
   return CA_OK;
 }
@@ -599,13 +757,15 @@ int launch_paged(const ca_cache_t& c, const ca_rows_t* Q, const void* K_pages, c
   prm.lse = lse;
   prm.k_pages = K_pages; prm.v_pages = V_pages;
   prm.lengths = lengths; prm.page_table = page_table;
-  prm.status = w.status; prm.units = w.units; prm.arrived = w.arrived; prm.partial = w.partial;
+  prm.status = w.status; prm.units = w.units; prm.partial = w.partial;
   prm.batch = c.batch; prm.heads_q = c.heads_q; prm.heads_kv = c.heads_kv; prm.group = c.heads_q / c.heads_kv;
   prm.page_rows = c.page_rows; prm.pages = c.pages; prm.pages_per_sequence = c.pages_per_sequence;
   prm.appended = appended; prm.left = c.left; prm.sinks = c.sinks;
   prm.scale_log2 = scale * 1.4426950408889634f;
-  if (c.dtype == CA_DTYPE_BF16)
-    return c.head_dim == 64 ? launch_paged_d<WarpMma<64>, 64>(prm, st) : launch_paged_d<WarpMma<128>, 128>(prm, st);
+  if (c.dtype == CA_DTYPE_BF16) {
+    if (row_tile(c) == 8) return c.head_dim == 64 ? launch_paged_d<WarpMma<64, 1>, 64>(prm, st) : launch_paged_d<WarpMma<128, 1>, 128>(prm, st);
+    return c.head_dim == 64 ? launch_paged_d<WarpMma<64, 2>, 64>(prm, st) : launch_paged_d<WarpMma<128, 2>, 128>(prm, st);
+  }
   auto fp32 = [&](auto rows) {
     constexpr int R = decltype(rows)::value;
     return c.head_dim == 64 ? launch_paged_d<WarpFma<64, R>, 64>(prm, st) : launch_paged_d<WarpFma<128, R>, 128>(prm, st);
