@@ -8,6 +8,7 @@ raise.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import math
 import os
@@ -466,12 +467,8 @@ def _rows(t: torch.Tensor, name: str, shape, dtype: torch.dtype, device: torch.d
     """A [batch, heads, rows, head_dim] tensor of that shape, type and device as the library takes it."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise ClusterAttnError(f"{name} must be a CUDA tensor (no CPU path exists)")
-    if t.device != device:
-        raise ClusterAttnError(f"{name} is on {t.device}, the call on {device}")
-    if t.dtype != dtype:
-        raise ClusterAttnError(f"{name} must be {dtype}, not {t.dtype}")
-    if tuple(t.shape) != tuple(shape):
-        raise ClusterAttnError(f"{name} must be {list(shape)}, not {list(t.shape)}")
+    if t.dtype != dtype or t.shape != shape or t.device != device:
+        raise ClusterAttnError(f"{name} must be {dtype} {list(shape)} on {device}, not {t.dtype} {list(t.shape)} on {t.device}")
     sb, sh, sn, sd = t.stride()
     if sd != 1:
         raise ClusterAttnError(f"{name}: the last dimension must be dense")
@@ -479,14 +476,14 @@ def _rows(t: torch.Tensor, name: str, shape, dtype: torch.dtype, device: torch.d
 
 
 def _int32(t: Optional[torch.Tensor], name: str, shape, device: torch.device):
-    """A dense int32 tensor of that shape, or None."""
+    """Address of a dense int32 tensor of that shape, or None."""
     if t is None:
         return None
-    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.device != device:
-        raise ClusterAttnError(f"{name} must be a CUDA tensor on {device}")
-    if t.dtype != torch.int32 or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+    if not isinstance(t, torch.Tensor) or t.device != device:
+        raise ClusterAttnError(f"{name} must be a tensor on {device}")
+    if t.dtype != torch.int32 or t.shape != shape or not t.is_contiguous():
         raise ClusterAttnError(f"{name} must be a contiguous int32 tensor {list(shape)}, not {t.dtype} {list(t.shape)}")
-    return ctypes.c_void_p(t.data_ptr())
+    return t.data_ptr()
 
 
 def _cuda_device(device) -> torch.device:
@@ -496,17 +493,25 @@ def _cuda_device(device) -> torch.device:
     return d if d.index is not None else torch.device("cuda", torch.cuda.current_device())
 
 
+# address of the current stream of a device; torch's own shortcut takes 0.1 us, the stream object 2.2
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
+
+
 def _call(fn, what: str, device: torch.device, stream: Optional[torch.cuda.Stream], *args) -> None:
     """A library call on `stream` (default: the device's current one) with the device current."""
-    if stream is not None and stream.device != device:
-        raise ClusterAttnError(f"{what}: the stream is on {stream.device}, the tensors on {device}")
-    handle = ctypes.c_void_p((stream if stream is not None else torch.cuda.current_stream(device)).cuda_stream)
+    if stream is None:
+        handle = _raw_stream(device.index)
+    else:
+        if stream.device != device:
+            raise ClusterAttnError(f"{what}: the stream is on {stream.device}, the tensors on {device}")
+        handle = stream.cuda_stream
     if torch.cuda.current_device() == device.index:
         rc = fn(*args, handle)
     else:
         with torch.cuda.device(device):
             rc = fn(*args, handle)
-    _check(rc, what)
+    if rc != CA_OK:
+        _check(rc, what)
 
 
 class Rotary:
@@ -530,10 +535,10 @@ class Rotary:
 
     def _positions(self, positions, batch: int, n: int, device: torch.device):
         """Pointer and batch stride of positions [batch, n, axes], or [1, n, axes] for the whole batch."""
+        if not isinstance(positions, torch.Tensor) or positions.dim() != 3:
+            raise ClusterAttnError("positions must be a [batch or 1, n, axes] tensor")
         axes = len(self.pairs)
-        shape = (1 if isinstance(positions, torch.Tensor) and positions.dim() == 3 and positions.shape[0] == 1 else batch, n, axes)
-        if positions is None:
-            raise ClusterAttnError("positions are missing")
+        shape = (1 if positions.shape[0] == 1 else batch, n, axes)
         return _int32(positions, "positions", shape, device), (0 if shape[0] == 1 else n * axes)
 
 
@@ -542,27 +547,33 @@ def rotary_axes(rotary: Rotary, q, k, positions, inverse: bool = False, out_q=No
     [batch or 1, n, axes] int32.  Returns (q', k'): new dense tensors, or out_q / out_k, which may be q and k."""
     if not isinstance(q, torch.Tensor) or q.dim() != 4 or q.dtype not in _OF_TORCH:
         raise ClusterAttnError("q must be a [batch, heads, n, head_dim] tensor of float32 or bfloat16")
-    device = _cuda_device(q.device)
-    B, H, n, D = q.shape
+    if not q.is_cuda:
+        raise ClusterAttnError("q must be a CUDA tensor (no CPU path exists)")
+    device, dtype, shape = q.device, q.dtype, q.shape
+    B, H, n, D = shape
     if D != rotary.head_dim:
         raise ClusterAttnError(f"q has head_dim {D}, the rotary positions {rotary.head_dim}")
-    if k is None and out_k is not None:
-        raise ClusterAttnError("out_k without k")
-    Hk = 0
+    pos, pos_b = rotary._positions(positions, B, n, device)
+    a, b, d, Hk = _rows(q, "q", shape, dtype, device), None, None, 0
     if k is not None:
         if not isinstance(k, torch.Tensor) or k.dim() != 4:
             raise ClusterAttnError("k must be a [batch, heads, n, head_dim] tensor")
         Hk = k.shape[1]
-    pos, pos_b = rotary._positions(positions, B, n, device)
+        shape_k = (B, Hk, n, D)
+        b = _rows(k, "k", shape_k, dtype, device)
+    elif out_k is not None:
+        raise ClusterAttnError("out_k without k")
     if out_q is None or (k is not None and out_k is None):
-        with torch.cuda.stream(stream):                    # new memory is in order with what the call's stream does (None: no change)
-            out_q = torch.empty((B, H, n, D), dtype=q.dtype, device=device) if out_q is None else out_q
-            out_k = torch.empty((B, Hk, n, D), dtype=q.dtype, device=device) if k is not None and out_k is None else out_k
-    a, c = _rows(q, "q", (B, H, n, D), q.dtype, device), _rows(out_q, "out_q", (B, H, n, D), q.dtype, device)
-    b = d = None
+        # new memory is in order with what the call's stream does
+        with contextlib.nullcontext() if stream is None else torch.cuda.stream(stream):
+            if out_q is None:
+                out_q = q.new_empty(shape)
+            if k is not None and out_k is None:
+                out_k = q.new_empty(shape_k)
+    c = _rows(out_q, "out_q", shape, dtype, device)
     if k is not None:
-        b, d = _rows(k, "k", (B, Hk, n, D), q.dtype, device), _rows(out_k, "out_k", (B, Hk, n, D), q.dtype, device)
-    _call(load_library().rotary_axes, "rotary_axes", device, stream, rotary._struct, B, H, Hk, n, D, _OF_TORCH[q.dtype],
+        d = _rows(out_k, "out_k", shape_k, dtype, device)
+    _call(load_library().rotary_axes, "rotary_axes", device, stream, rotary._struct, B, H, Hk, n, D, _OF_TORCH[dtype],
           1 if inverse else 0, a, b, pos, pos_b, c, d)
     return out_q, out_k
 
@@ -587,29 +598,27 @@ class PagedCache:
         _check(lib.ca_cache_workspace_bytes(ctypes.byref(p), ctypes.byref(size)), "ca_cache_workspace_bytes")
         self.dtype = _TORCH[p.dtype]
         pool = (p.pages, p.heads_kv, p.page_rows, p.head_dim)
-        self.K_pages = torch.zeros(pool, dtype=self.dtype, device=dev) if K_pages is None else K_pages
-        self.V_pages = torch.zeros(pool, dtype=self.dtype, device=dev) if V_pages is None else V_pages
-        self.page_table = (torch.zeros((p.batch, p.pages_per_sequence), dtype=torch.int32, device=dev)
-                           if page_table is None else page_table)
-        self.lengths = torch.zeros((p.batch,), dtype=torch.int32, device=dev) if lengths is None else lengths
-        self._pools()
-        self._indices()
+        self._K_pages = torch.zeros(pool, dtype=self.dtype, device=dev) if K_pages is None else K_pages
+        self._V_pages = torch.zeros(pool, dtype=self.dtype, device=dev) if V_pages is None else V_pages
+        self._page_table = (torch.zeros((p.batch, p.pages_per_sequence), dtype=torch.int32, device=dev)
+                            if page_table is None else page_table)
+        self._lengths = torch.zeros((p.batch,), dtype=torch.int32, device=dev) if lengths is None else lengths
+        for name, t in (("K_pages", self._K_pages), ("V_pages", self._V_pages)):
+            _rows(t, name, pool, self.dtype, dev)
+            if not t.is_contiguous():
+                raise ClusterAttnError(f"{name} must be contiguous")
+        for name, t, shape in (("lengths", self._lengths, (p.batch,)), ("page_table", self._page_table, (p.batch, p.pages_per_sequence))):
+            if _int32(t, name, shape, dev) is None:
+                raise ClusterAttnError(f"{name} is missing")
         self.O = torch.zeros((p.batch, p.heads_q, 1, p.head_dim), dtype=self.dtype, device=dev)
         self.lse = torch.zeros((p.batch, p.heads_q, 1), dtype=torch.float32, device=dev)
         self.ws = torch.zeros(size.value, dtype=torch.uint8, device=dev)
 
-    def _pools(self):
-        p = self.problem
-        for name, t in (("K_pages", self.K_pages), ("V_pages", self.V_pages)):
-            _rows(t, name, (p.pages, p.heads_kv, p.page_rows, p.head_dim), self.dtype, self.device)
-            if not t.is_contiguous():
-                raise ClusterAttnError(f"{name} must be contiguous")
-        return _ptr(self.K_pages), _ptr(self.V_pages)
-
-    def _indices(self):
-        p = self.problem
-        return (_int32(self.lengths, "lengths", (p.batch,), self.device),
-                _int32(self.page_table, "page_table", (p.batch, p.pages_per_sequence), self.device))
+    # the tensors of the cache: written into by the program, and the same ones for the life of the cache
+    K_pages = property(lambda self: self._K_pages)
+    V_pages = property(lambda self: self._V_pages)
+    page_table = property(lambda self: self._page_table)
+    lengths = property(lambda self: self._lengths)
 
     def cache_append(self, K, V, count=None, rotary: Optional[Rotary] = None, positions=None, stream=None):
         """cache_append of the C library: rows of K and V [batch, heads_kv, n, head_dim] (of sequence b the first
@@ -628,10 +637,9 @@ class PagedCache:
             rot = rotary._struct
         elif positions is not None:
             raise ClusterAttnError("positions without rotary")
-        lengths, table = self._indices()
-        kp, vp = self._pools()
-        _call(load_library().cache_append, "cache_append", self.device, stream, p, n, k, v, lengths,
-              _int32(count, "count", (p.batch,), self.device), table, rot, pos, pos_b, kp, vp, _ptr(self.ws), self.ws.numel())
+        _call(load_library().cache_append, "cache_append", self.device, stream, p, n, k, v, self._lengths.data_ptr(),
+              _int32(count, "count", (p.batch,), self.device), self._page_table.data_ptr(), rot, pos, pos_b, self._K_pages.data_ptr(),
+              self._V_pages.data_ptr(), self.ws.data_ptr(), self.ws.numel())
 
     def paged_attention_fwd(self, Q, appended: int = 0, out=None, want_lse: bool = True, stream=None):
         """paged_attention_fwd of the C library: Q [batch, heads_q, 1, head_dim] against lengths[b] + appended
@@ -640,11 +648,9 @@ class PagedCache:
         shape = (p.batch, p.heads_q, 1, p.head_dim)
         out = self.O if out is None else out
         q, o = _rows(Q, "Q", shape, self.dtype, self.device), _rows(out, "out", shape, self.dtype, self.device)
-        lengths, table = self._indices()
-        kp, vp = self._pools()
         lse = self.lse if want_lse else None
-        _call(load_library().paged_attention_fwd, "paged_attention_fwd", self.device, stream, p, q, kp, vp, lengths,
-              int(appended), table, o, _ptr(lse), _ptr(self.ws), self.ws.numel())
+        _call(load_library().paged_attention_fwd, "paged_attention_fwd", self.device, stream, p, q, self._K_pages.data_ptr(),
+              self._V_pages.data_ptr(), self._lengths.data_ptr(), int(appended), self._page_table.data_ptr(), o, None if lse is None else lse.data_ptr(), self.ws.data_ptr(), self.ws.numel())
         return out, lse
 
     def last_status(self) -> int:
@@ -682,8 +688,8 @@ class WindowPlan:
         o = _rows(out, "out", (p.batch, p.heads_q, p.n_q, p.head_dim), dt, dev)
         lse = self.lse if want_lse else None
         _call(load_library().window_attention_fwd, "window_attention_fwd", dev, stream, p, q, k, v,
-              _int32(len_q, "len_q", (p.batch,), dev), _int32(len_k, "len_k", (p.batch,), dev), o, _ptr(lse), _ptr(self.ws),
-              self.ws.numel())
+              _int32(len_q, "len_q", (p.batch,), dev), _int32(len_k, "len_k", (p.batch,), dev), o,
+              None if lse is None else lse.data_ptr(), self.ws.data_ptr(), self.ws.numel())
         return out, lse
 
     def last_status(self) -> int:

@@ -31,7 +31,6 @@ struct RowSet {
   void* out;
   long long in_b, in_h, in_n, out_b, out_h, out_n;
   int heads;
-  int rotate;
 };
 
 struct RotaryParams {
@@ -42,6 +41,7 @@ struct RotaryParams {
   // pages (kPaged): out is a pool [pages][heads][page_rows][D]
   const int32_t *lengths, *count, *page_table;
   int page_rows, pages, pages_per_sequence, batch;
+  long long lines;                           // rows of all batch items
   int* status;
 };
 
@@ -74,14 +74,102 @@ __device__ __forceinline__ void turn(T& x, T& y, float c, float s) {
 }
 
 // An item of a row: a vector of it, or with halves a vector of the first half and its partner.  Threads of a
-// block: rows_per_block rows by the items of a row; blockIdx.y: heads; blockIdx.z: batch.
+// block: rows_per_block rows by the items of a row; blockIdx.y: heads.
+template <typename T, int D, int PAIRS, bool PAGED>
+__device__ __forceinline__ void rotary_rows(const unsigned long long* s_turns, const unsigned char* s_axis, int pairs, int axes,
+                                            const RotaryParams& prm) {
+  constexpr int W = PAIRS == kHalvesScalar ? 1 : 16 / (int)sizeof(T);
+  constexpr bool HALVES = PAIRS == kHalves || PAIRS == kHalvesScalar;
+  constexpr int ANGLES = PAIRS == kNoPairs ? 1 : HALVES ? W : W / 2;
+  const int item = threadIdx.x % prm.items, sub = threadIdx.x / prm.items;
+  const long long line = (long long)blockIdx.x * prm.rows_per_block + sub;     // of all batch items
+  if (sub >= prm.rows_per_block || line >= prm.lines) return;
+  const int b = prm.lines <= 0xffffffffLL ? (int)((unsigned)line / (unsigned)prm.n) : (int)(line / prm.n);
+  const long long row = line - (long long)b * prm.n;
+
+  long long slot = 0;                                    // first element of the row's place in a pool, of head 0
+  if (PAGED) {
+    const int start = prm.lengths[b], count = prm.count ? prm.count[b] : prm.n;
+    if (start < 0 || row >= count) return;               // (a row that is not there)
+    const unsigned at = (unsigned)start + (unsigned)row, page = at / (unsigned)prm.page_rows;
+    if (page >= (unsigned)prm.pages_per_sequence) return;
+    const int id = prm.page_table[(size_t)b * prm.pages_per_sequence + page];
+    if ((unsigned)id >= (unsigned)prm.pages) return;
+    slot = ((long long)id * prm.set[0].heads * prm.page_rows + at % (unsigned)prm.page_rows) * D;
+  }
+
+  const int R = PAIRS == kNoPairs ? 0 : pairs;
+  const int lead = HALVES ? R / W : 0;                   // items with a partner
+  const bool both = HALVES && item < lead;
+  const int first = !HALVES ? item * W : both ? item * W : 2 * R + (item - lead) * W;
+  const int begin = blockIdx.y * prm.heads_per_thread, heads0 = prm.set[0].heads;
+  const int end = min(begin + prm.heads_per_thread, heads0 + prm.set[1].heads);
+
+  // ---- heads, four at a time
+  using V = typename Vec<T, W>::type;
+  constexpr int N = 4;
+  Pack<T, W> x[N], y[N];
+  auto load = [&](int h) {
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      if (h + j >= end) break;
+      const RowSet& set = prm.set[h + j < heads0 ? 0 : 1];
+      const T* in = static_cast<const T*>(set.in) + b * set.in_b + row * set.in_n + (h + j - (h + j < heads0 ? 0 : heads0)) * set.in_h + first;
+      x[j].raw = *reinterpret_cast<const V*>(in);
+      if (both) y[j].raw = *reinterpret_cast<const V*>(in + R);
+    }
+  };
+  load(begin);                                           // on their way while the angles are computed
+
+  // ---- sines and cosines of this thread's pairs; a pair behind the last one stays as it is
+  float cs[ANGLES], sn[ANGLES];
+  int turned = 0;
+  if (PAIRS != kNoPairs) {
+    const int32_t* pos = prm.positions + b * prm.pos_b + row * axes;
+    const int pair0 = HALVES ? item * W : item * (W / 2);
+#pragma unroll
+    for (int i = 0; i < ANGLES; ++i) {
+      const int pair = pair0 + i;
+      cs[i] = 1.f;
+      sn[i] = 0.f;
+      if (pair < R) {
+        const unsigned long long phase = (unsigned long long)(long long)pos[s_axis[pair]] * s_turns[pair];
+        sincospif((float)(long long)phase * 0x1p-63f, &sn[i], &cs[i]);
+        if (prm.inverse) sn[i] = -sn[i];
+        turned = i + 1;
+      }
+    }
+  }
+  for (int h = begin; h < end; h += N) {
+    if (h > begin) load(h);
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      if (h + j >= end) break;
+      const int which = h + j < heads0 ? 0 : 1, head = h + j - (which ? heads0 : 0);
+      const RowSet& set = prm.set[which];
+      if (PAIRS != kNoPairs && (!PAGED || which == 0)) { // (of rows for a cache the second set are values)
+        if (HALVES) {
+          if (both) {
+#pragma unroll
+            for (int i = 0; i < ANGLES; ++i) turn(x[j].e[i], y[j].e[i], cs[i], sn[i]);
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < ANGLES; ++i)
+            if (i < turned) turn(x[j].e[2 * i % W], x[j].e[(2 * i + 1) % W], cs[i], sn[i]);
+        }
+      }
+      T* out = static_cast<T*>(set.out) + first + (PAGED ? slot + (long long)head * prm.page_rows * D : b * set.out_b + row * set.out_n + head * set.out_h);
+      *reinterpret_cast<V*>(out) = x[j].raw;
+      if (both) *reinterpret_cast<V*>(out + R) = y[j].raw;
+    }
+  }
+}
+
 template <typename T, int D, int PAIRS, bool PAGED>
 __global__ void __launch_bounds__(256) rotary_kernel(const __grid_constant__ RotaryTable table,
                                                      const __grid_constant__ RotaryParams prm) {
   wait_for_previous();
-  constexpr int W = PAIRS == kHalvesScalar ? 1 : 16 / (int)sizeof(T);
-  constexpr bool HALVES = PAIRS == kHalves || PAIRS == kHalvesScalar;
-  constexpr int ANGLES = PAIRS == kNoPairs ? 1 : HALVES ? W : W / 2;
   __shared__ unsigned long long s_turns[kMaxPairs];
   __shared__ unsigned char s_axis[kMaxPairs];
   if (PAIRS != kNoPairs) {
@@ -92,8 +180,8 @@ __global__ void __launch_bounds__(256) rotary_kernel(const __grid_constant__ Rot
     __syncthreads();
   }
   let_next_start();
-  const int b = blockIdx.z;
-  if (PAGED && blockIdx.x == 0 && blockIdx.y == 0 && b == 0) {
+  rotary_rows<T, D, PAIRS, PAGED>(s_turns, s_axis, table.pairs, table.axes, prm);
+  if (PAGED && blockIdx.x == 0 && blockIdx.y == 0) {
     // This block looks at every index of the call and writes the status word, so that nothing has to clear it first.
     int bad = 0;
     const int most = prm.n / prm.page_rows + 2;
@@ -110,86 +198,6 @@ __global__ void __launch_bounds__(256) rotary_kernel(const __grid_constant__ Rot
     bad = __syncthreads_or(bad);
     if (threadIdx.x == 0) *prm.status = bad ? CA_ERR_BAD_INDEX : CA_OK;
   }
-  const int item = threadIdx.x % prm.items, sub = threadIdx.x / prm.items;
-  const long long row = (long long)blockIdx.x * prm.rows_per_block + sub;
-  if (sub >= prm.rows_per_block || row >= prm.n) return;
-
-  long long slot = 0;                                    // first element of the row's place in a pool, of head 0
-  if (PAGED) {
-    const int start = prm.lengths[b], count = prm.count ? prm.count[b] : prm.n;
-    if (start < 0 || row >= count) return;               // (a row that is not there)
-    const long long at = start + row, page = at / prm.page_rows;
-    if (page >= prm.pages_per_sequence) return;
-    const int id = prm.page_table[(size_t)b * prm.pages_per_sequence + page];
-    if ((unsigned)id >= (unsigned)prm.pages) return;
-    slot = ((long long)id * prm.set[0].heads * prm.page_rows + at % prm.page_rows) * D;
-  }
-
-  // ---- sines and cosines of this thread's pairs; a pair behind the last one stays as it is
-  const int R = PAIRS == kNoPairs ? 0 : table.pairs;
-  const int lead = HALVES ? R / W : 0;                   // items with a partner
-  const bool both = HALVES && item < lead;
-  const int first = !HALVES ? item * W : both ? item * W : 2 * R + (item - lead) * W;
-  const int partner = first + R;
-  float cs[ANGLES], sn[ANGLES];
-  int turned = 0;
-  if (PAIRS != kNoPairs) {
-    const int32_t* pos = prm.positions + b * prm.pos_b + row * table.axes;
-    const int pair0 = HALVES ? item * W : item * (W / 2);
-#pragma unroll
-    for (int i = 0; i < ANGLES; ++i) {
-      const int pair = pair0 + i;
-      cs[i] = 1.f;
-      sn[i] = 0.f;
-      if (pair < R) {
-        const unsigned long long phase = (unsigned long long)(long long)pos[s_axis[pair]] * s_turns[pair];
-        sincospif((float)(long long)phase * 0x1p-63f, &sn[i], &cs[i]);
-        if (prm.inverse) sn[i] = -sn[i];
-        turned = i + 1;
-      }
-    }
-  }
-
-  auto go = [&](const RowSet& set, int h0, int h1, bool rotate) {
-    using P = Pack<T, W>;
-    const T* in = static_cast<const T*>(set.in) + b * set.in_b + row * set.in_n + first;
-    T* out = static_cast<T*>(set.out) + (PAGED ? slot : b * set.out_b + row * set.out_n) + first;
-    const long long out_h = PAGED ? (long long)prm.page_rows * D : set.out_h;
-    auto some = [&](int h, auto count) {
-      constexpr int N = decltype(count)::value;
-      P x[N], y[N];
-#pragma unroll
-      for (int j = 0; j < N; ++j) {
-        x[j].raw = *reinterpret_cast<const typename Vec<T, W>::type*>(in + (h + j) * set.in_h);
-        if (both) y[j].raw = *reinterpret_cast<const typename Vec<T, W>::type*>(in + (h + j) * set.in_h + (partner - first));
-      }
-#pragma unroll
-      for (int j = 0; j < N; ++j) {
-        if (PAIRS != kNoPairs && rotate) {
-          if (HALVES) {
-            if (both) {
-#pragma unroll
-              for (int i = 0; i < ANGLES; ++i) turn(x[j].e[i], y[j].e[i], cs[i], sn[i]);
-            }
-          } else {
-#pragma unroll
-            for (int i = 0; i < ANGLES; ++i)
-              if (i < turned) turn(x[j].e[2 * i % W], x[j].e[(2 * i + 1) % W], cs[i], sn[i]);
-          }
-        }
-        *reinterpret_cast<typename Vec<T, W>::type*>(out + (h + j) * out_h) = x[j].raw;
-        if (both) *reinterpret_cast<typename Vec<T, W>::type*>(out + (h + j) * out_h + (partner - first)) = y[j].raw;
-      }
-    };
-    int h = h0;
-    for (; h + 4 <= h1; h += 4) some(h, std::integral_constant<int, 4>{});
-    for (; h < h1; ++h) some(h, std::integral_constant<int, 1>{});
-  };
-  const int begin = blockIdx.y * prm.heads_per_thread;
-  const int end = min(begin + prm.heads_per_thread, prm.set[0].heads + prm.set[1].heads);
-  const int mid = min(max(prm.set[0].heads, begin), end);
-  if (begin < mid) go(prm.set[0], begin, mid, prm.set[0].rotate != 0);
-  if (mid < end) go(prm.set[1], mid - prm.set[0].heads, end - prm.set[0].heads, prm.set[1].rotate != 0);
 }
 
 // ---- host side -------------------------------------------------------------------------------------------
@@ -243,13 +251,15 @@ static int launch_rotary_d(const RotaryTable& table, RotaryParams& prm, int pair
   prm.items = pairs_mode == kHalves || pairs_mode == kHalvesScalar ? D / w - R / w : D / W;
   prm.rows_per_block = 256 / prm.items;
   const int heads = prm.set[0].heads + prm.set[1].heads;
-  const long long blocks_n = ((long long)prm.n + prm.rows_per_block - 1) / prm.rows_per_block;
+  prm.batch = batch;
+  prm.lines = (long long)prm.n * batch;
+  const long long blocks_n = (prm.lines + prm.rows_per_block - 1) / prm.rows_per_block;
   // heads per thread: its sines and cosines serve 8, fewer where that leaves SMs without blocks
   int per = 8;
-  while (per > 1 && blocks_n * batch * ((heads + per - 1) / per) < 2 * 148) per /= 2;
+  while (per > 1 && blocks_n * ((heads + per - 1) / per) < 2 * 148) per /= 2;
   prm.heads_per_thread = per;
-  const dim3 grid((unsigned)blocks_n, (unsigned)((heads + per - 1) / per), (unsigned)batch);
-  if (blocks_n > 0x7fffffffLL || grid.y > 65535u || batch > 65535) return CA_ERR_UNSUPPORTED;
+  const dim3 grid((unsigned)blocks_n, (unsigned)((heads + per - 1) / per));
+  if (blocks_n > 0x7fffffffLL || grid.y > 65535u) return CA_ERR_UNSUPPORTED;
   auto go = [&](auto mode) -> int {
     launch_chained(rotary_kernel<T, D, decltype(mode)::value, PAGED>, grid, 256, 0, st, table, prm);
     CA_LAUNCH_CHECK();
@@ -285,7 +295,7 @@ int check_rows(const ca_rows_t* x, int batch, int heads, int n, int D, int dtype
   return CA_OK;
 }
 
-static RowSet row_set(const ca_rows_t* in, const ca_rows_t* out, int heads, int rotate) {
+static RowSet row_set(const ca_rows_t* in, const ca_rows_t* out, int heads) {
   RowSet s{};
   s.in = in->data;
   s.in_b = in->stride_b; s.in_h = in->stride_h; s.in_n = in->stride_n;
@@ -294,7 +304,6 @@ static RowSet row_set(const ca_rows_t* in, const ca_rows_t* out, int heads, int 
     s.out_b = out->stride_b; s.out_h = out->stride_h; s.out_n = out->stride_n;
   }
   s.heads = heads;
-  s.rotate = rotate;
   return s;
 }
 
@@ -305,8 +314,8 @@ int launch_rotary_axes(const ca_rotary_t& rot, int batch, int heads_q, int heads
   const int rc = make_table(rot, D, &table);
   if (rc != CA_OK) return rc;
   RotaryParams prm{};
-  if (heads_q) prm.set[0] = row_set(Q, Qo, heads_q, 1);
-  if (heads_k) prm.set[1] = row_set(K, Ko, heads_k, 1);
+  if (heads_q) prm.set[0] = row_set(Q, Qo, heads_q);
+  if (heads_k) prm.set[1] = row_set(K, Ko, heads_k);
   prm.positions = positions;
   prm.pos_b = pos_b;
   prm.n = n;
@@ -323,8 +332,8 @@ int launch_cache_append(const ca_cache_t& c, int n, const ca_rows_t* K, const ca
     if (rc != CA_OK) return rc;
   }
   RotaryParams prm{};
-  prm.set[0] = row_set(K, nullptr, c.heads_kv, 1);
-  prm.set[1] = row_set(V, nullptr, c.heads_kv, 0);
+  prm.set[0] = row_set(K, nullptr, c.heads_kv);
+  prm.set[1] = row_set(V, nullptr, c.heads_kv);
   prm.set[0].out = K_pages;
   prm.set[1].out = V_pages;
   prm.positions = positions;

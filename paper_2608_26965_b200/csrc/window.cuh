@@ -11,14 +11,16 @@ struct WindowParams {
   float* lse;                       // [batch][heads_q][n_q] or null
   const int32_t *len_q, *len_k;     // [batch] or null
   int* status;
-  int32_t* redo;                    // [batch * heads_q][blocks of kWindowBlock rows][16]: two words for 32 rows, to be computed again if one is set (null: all)
-  int32_t* redo_any;                // whether there are any
+  int32_t* pieces;                  // [batch + 1] blocks of kWindowBlock rows of the batch items before
+  int32_t* redo;                    // [batch * heads_q][blocks of kWindowBlock rows][8]: 32 rows each, to be computed again (null: all)
   int batch, heads_q, heads_kv, group, n_q, n_k, left, right, sinks;
   float scale_log2;
 };
 
 constexpr int kWindowTile = 128;    // query rows of a tensor-core tile
 constexpr int kWindowBlock = 256;   // two of them: what a CTA works on at a time
+// words of the status block behind the status: a counter that hands out work, whether rows are to be computed again
+constexpr int kNextWord = kTileWord, kRedoWord = kTileWord + 1;
 
 // Lengths of a batch item, kept in range (what is out of it is flagged by check_lengths).
 struct WindowItem {
@@ -66,6 +68,6 @@ struct WindowRow {
 };
 
 int launch_window_ref(const WindowParams& prm, int D, int dtype, LaunchStream st);
-int launch_window_tc(const WindowParams& prm, int D, int* next, LaunchStream st);    // CA_ERR_UNSUPPORTED: strides that it does not take
+int launch_window_tc(const WindowParams& prm, int D, LaunchStream st);    // CA_ERR_UNSUPPORTED: strides that it does not take
 
 }  // namespace ca

@@ -35,16 +35,16 @@ __global__ void __launch_bounds__(kWrThreads) window_ref_kernel(const __grid_con
   float* sv = sk + kWrKeys * (D + 4);
   float* sp = sv + kWrKeys * (D + 4);           // [64][68]
   const int tid = threadIdx.x, ty = tid >> 4, tx = tid & 15;
-  if (blockIdx.x == 0) {
+  if (prm.redo) {
+    if (prm.status[kRedoWord] == 0) return;
+  } else if (blockIdx.x == 0) {
+    // the only one that writes the status word
     int bad = 0;
     for (int i = tid; i < prm.batch; i += kWrThreads)
       bad |= (prm.len_q && (unsigned)prm.len_q[i] > (unsigned)prm.n_q) || (prm.len_k && (unsigned)prm.len_k[i] > (unsigned)prm.n_k);
     bad = __syncthreads_or(bad);
-    // the only one that writes the status word, unless the tensor-core kernel has recorded something
-    if (tid == 0 && !prm.redo) *prm.status = bad ? CA_ERR_BAD_INDEX : CA_OK;
-    if (tid == 0 && prm.redo && bad) atomicCAS(prm.status, 0, CA_ERR_BAD_INDEX);
+    if (tid == 0) *prm.status = bad ? CA_ERR_BAD_INDEX : CA_OK;
   }
-  if (prm.redo && *prm.redo_any == 0) return;
   const int blocks64 = (prm.n_q + kWrRows - 1) / kWrRows;
   const long long n_work = (long long)blocks64 * prm.heads_q * prm.batch;
 #pragma unroll 1
@@ -53,8 +53,8 @@ __global__ void __launch_bounds__(kWrThreads) window_ref_kernel(const __grid_con
   const WindowItem it(prm, b);
   if (r0 >= it.len_q) continue;
   if (prm.redo) {
-    const int32_t* marks = prm.redo + ((size_t)bh * ((prm.n_q + kWindowBlock - 1) / kWindowBlock) + r0 / kWindowBlock) * 16 + r0 % kWindowBlock / 16;
-    if ((marks[0] | marks[1] | marks[2] | marks[3]) == 0) continue;
+    const int32_t* marks = prm.redo + ((size_t)bh * ((prm.n_q + kWindowBlock - 1) / kWindowBlock) + r0 / kWindowBlock) * 8 + r0 % kWindowBlock / 32;
+    if ((marks[0] | marks[1]) == 0) continue;
   }
   const int rows = min(kWrRows, it.len_q - r0);
   const WindowSpan span(prm, it, r0, r0 + rows, kWrKeys);
@@ -190,8 +190,8 @@ int launch_window_ref(const WindowParams& prm, int D, int dtype, LaunchStream st
 }
 
 size_t window_workspace_bytes(const ca_window_t& p) {
-  // status block, marks of the rows to compute again
-  return kStatusBytes + align_up((size_t)p.batch * p.heads_q * ceil_div(p.n_q, kWindowBlock) * 16 * sizeof(int32_t), 256);
+  // status block, blocks of rows of every batch item, marks of the rows to compute again
+  return kStatusBytes + align_up(((size_t)p.batch + 1) * sizeof(int32_t), 256) + align_up((size_t)p.batch * p.heads_q * ceil_div(p.n_q, kWindowBlock) * 8 * sizeof(int32_t), 256);
 }
 
 int launch_window(const ca_window_t& p, const ca_rows_t* Q, const ca_rows_t* K, const ca_rows_t* V, const int32_t* len_q,
@@ -208,10 +208,11 @@ int launch_window(const ca_window_t& p, const ca_rows_t* Q, const ca_rows_t* K, 
   prm.n_q = p.n_q; prm.n_k = p.n_k; prm.left = p.left; prm.right = p.right; prm.sinks = p.sinks;
   prm.scale_log2 = scale * 1.4426950408889634f;
   if (p.dtype == CA_DTYPE_BF16 && !(p.flags & CA_ATTN_FP32)) {
-    int* status = static_cast<int*>(ws);
-    prm.redo = status + kStatusBytes / sizeof(int);
-    prm.redo_any = status + kTileWord + 1;
-    const int rc = launch_window_tc(prm, p.head_dim, status + kTileWord, st);
+    Carver c(ws);
+    c.take<int>(kStatusBytes / sizeof(int));
+    prm.pieces = c.take<int32_t>((size_t)p.batch + 1);
+    prm.redo = c.take<int32_t>((size_t)p.batch * p.heads_q * ceil_div(p.n_q, kWindowBlock) * 8);
+    const int rc = launch_window_tc(prm, p.head_dim, st);
     if (rc == CA_OK) return launch_window_ref(prm, p.head_dim, p.dtype, st);
     if (rc != CA_ERR_UNSUPPORTED) return rc;
     prm.redo = nullptr;                         // strides of a broadcast: on the CUDA cores

@@ -3,18 +3,29 @@
 // A CTA (one per SM, persistent) works on 256 query rows of a head at a time, two tiles of 128, which share the key and
 // value tiles of 128 rows that they see: the first tokens' tiles, then the window's.  For each of the two and every key tile
 //     S  = Q K^T           tcgen05.mma, Q and K in shared memory
-//     P  = exp2(S c - m)   one query row per thread, so that maximum and sum need no other thread; P goes back over S in
-//                          tensor memory as bf16
+//     P  = exp2(S c - m)   one query row per thread, so that its sum needs no other thread; P goes back over S in
+//                          tensor memory as bf16, and its first half is handed to the products before the second is computed
 //     O += P V             tcgen05.mma, P from tensor memory
 // and while four warps are at the softmax of one tile, the tensor core is at the products of the other.  Roles: warp 0 loads (TMA, 128-byte
 // swizzle), one thread of warp 1 issues the products, warp 2 sets value rows behind the last key to zero, warp 3 hands out work,
 // warps 4-7 and 8-11 are the softmax of the two query tiles.  All of them run ahead of one another across pieces of work.
 //
-// m is the running maximum, moved only when the new one is 2^8 larger: until then P is at most 2^8 and nothing
-// needs rescaling (P is bf16, O and the sum are fp32: no precision is lost).
-// Masks: only key tiles at a border of a row's window are masked, by selecting scores before the maximum.  A masked P is 0, and
+// m is not the running maximum but a reference that keeps exp2 in range: the maximum of the first keys that a row sees, raised (by a
+// whole number, at the next step) when a sum of 32 probabilities exceeded 2^32.  P is bf16, O and the sum are fp32, so
+// that probabilities far above 1 cost no precision, and no pass over the scores for their maximum stands between S and P.
+// Masks: only key tiles at a border of a row's window are masked, by selecting scores.  A masked P is 0, and
 // 0 x infinity is not: rows whose result is not finite are marked and computed again on the CUDA cores, where
-// what is masked takes no part and no P is above 1 (a second launch, which ends at once when no row is marked).
+// what is masked takes no part and no P is above 1 (a launch of its own, which ends at once when no row is marked).
+//
+// What bounds it: a step (256 x 128 scores, d = 128) takes some 3,200 cycles.  The products take 2,650 of them, 2,048 if shared
+// memory fed both operands of Q K^T without a pause (they need all of its 128 bytes a cycle, and the loads of the next tiles and V
+// come on top); the exponentials 1,900 of the special-function unit's time.  Between the two lies the chain S -> P -> O of each
+// query tile.  Calls in a row are bound by power: 40 heads of 32,760 rows, d = 128, two frames of 1,560 to either side and the first
+// one take 4.10 ms by themselves and 4.65 in a row (1.06 PFLOP/s of visible pairs, 1.18 with the masked parts of tiles; plain
+// products of 8,192^3 1.41 in a row).  Tried and slower: 16 softmax warps with half of a row's columns each (4.40 ms), the
+// issuing thread looking at barriers without a pause (5.27: its looks delay everybody's), a pass for the exact maximum (4.17),
+// every eighth instead of every sixteenth pair of exponentials on the FMA units (4.26; none 4.09, but 476 us instead of 452 at d = 64,
+// 8 heads of 18,944 rows).
 #include <math.h>
 
 #include "tc_ptx.cuh"
@@ -30,9 +41,11 @@ constexpr int kWtKeys = 128;
 
 
 
-constexpr int kWtEvery = 8;                // one pair of columns in eight takes its exponentials from the FMA units
+constexpr int kWtEvery = 16;               // of every 16 columns, two take their exponentials from the FMA units
 constexpr float kE1 = 0.693147004f, kE2 = 0.240222424f, kE3 = 0.0555073358f, kE4 = 0.00967151299f, kE5 = 0.00132647273f;
-constexpr float kWtRaise = 8.f;            // log2 units that a row's scores may climb above its reference
+constexpr float kWtSumLimit = 4294967296.f;   // 2^32: a sum of 32 probabilities above it raises the reference
+
+constexpr int kWtRing = 4;                 // pieces of work on their way
 
 template <int D>
 struct WtCfg {
@@ -41,9 +54,9 @@ struct WtCfg {
   static constexpr int TILE_BYTES = PANELS * PANEL_BYTES;     // 128 rows
   static constexpr int NK = D == 128 ? 2 : 4, NV = D == 128 ? 3 : 4;
   static constexpr int OFF_Q = 0, OFF_K = 2 * TILE_BYTES, OFF_V = OFF_K + NK * TILE_BYTES;
-  static constexpr int OFF_WORK = OFF_V + NV * TILE_BYTES;    // [2] Work
-  static constexpr int OFF_BAR = OFF_WORK + 2 * 64;
-  static constexpr int NUM_BARS = 20 + 2 * NK + 3 * NV;
+  static constexpr int OFF_WORK = OFF_V + NV * TILE_BYTES;    // [kWtRing] Work
+  static constexpr int OFF_BAR = OFF_WORK + kWtRing * 64;
+  static constexpr int NUM_BARS = 16 + 2 * kWtRing + 2 * NK + 3 * NV;
   static constexpr int OFF_MISC = OFF_BAR + 8 * NUM_BARS;     // tensor memory base, abort flag
   static constexpr int SMEM = 1024 + OFF_MISC + 16;
   static_assert(SMEM <= 227 * 1024, "shared memory");
@@ -56,9 +69,8 @@ struct Work {
   int pad[4];
   __device__ __forceinline__ int tile(int u) const { return u < sink_tiles ? u : tile_lo + u - sink_tiles; }
   // whether query tile i takes part in the step of key tile t
-  __device__ __forceinline__ bool active(int i, int t, int sinks) const { return takes_part(lo[i], hi[i], t, sinks); }
-  __device__ __forceinline__ static bool takes_part(int lo, int hi, int t, int sinks) {
-    const int k0 = t * kWtKeys;
+  __device__ __forceinline__ bool active(int i, int t, int sinks) const { return takes_part(lo[i], hi[i], t * kWtKeys, sinks); }
+  __device__ __forceinline__ static bool takes_part(int lo, int hi, int k0, int sinks) {
     return k0 < hi && (k0 + kWtKeys > lo || k0 < sinks);
   }
 };
@@ -66,9 +78,9 @@ static_assert(sizeof(Work) == 64, "a work slot");
 
 struct WtParams {
   WindowParams w;
-  int* next;                               // counter that hands out work, zero at the start
-  int blocks, n_work;                      // pieces of a head, of the call
+  int blocks, rows_first;                  // blocks of a head; order of the pieces
   long long wait_limit;
+  int wide;                                // rows of O start at 32-byte boundaries
 };
 
 __device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map, int x, int y, int z, int w, uint32_t bar) {
@@ -76,6 +88,44 @@ __device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map
       "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
       ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(w), "r"(bar)
       : "memory");
+}
+
+// Blocks of rows before each batch item, counters and status: one CTA.
+__global__ void __launch_bounds__(256) window_prepare_kernel(const __grid_constant__ WindowParams prm) {
+  wait_for_previous();
+  let_next_start();
+  __shared__ int warp_sum[8];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  int bad = 0, before = 0;
+  for (int base = 0; base < prm.batch; base += 256) {
+    const int b = base + tid;
+    int v = 0;
+    if (b < prm.batch) {
+      bad |= (prm.len_q && (unsigned)prm.len_q[b] > (unsigned)prm.n_q) || (prm.len_k && (unsigned)prm.len_k[b] > (unsigned)prm.n_k);
+      v = (WindowItem(prm, b).len_q + kWindowBlock - 1) / kWindowBlock;
+    }
+    for (int d = 1; d < 32; d <<= 1) {
+      const int o = __shfl_up_sync(0xffffffffu, v, d);
+      if (lane >= d) v += o;
+    }
+    if (lane == 31) warp_sum[warp] = v;
+    __syncthreads();
+    int all = 0;
+    for (int w = 0; w < 8; ++w) {
+      if (w < warp) v += warp_sum[w];
+      all += warp_sum[w];
+    }
+    if (b < prm.batch) prm.pieces[b + 1] = before + v;
+    before += all;
+    __syncthreads();
+  }
+  bad = __syncthreads_or(bad);
+  if (tid == 0) {
+    prm.pieces[0] = 0;
+    prm.status[0] = bad ? CA_ERR_BAD_INDEX : CA_OK;
+    prm.status[kNextWord] = 0;
+    prm.status[kRedoWord] = 0;
+  }
 }
 
 __device__ __forceinline__ f32x2 exp2_unit(f32x2 x) {
@@ -118,17 +168,17 @@ window_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
   const uint32_t s_q = s_base + C::OFF_Q, s_k = s_base + C::OFF_K, s_v = s_base + C::OFF_V;
   volatile Work* work_ring = reinterpret_cast<volatile Work*>(smem + C::OFF_WORK);
   const uint32_t bar0 = s_base + C::OFF_BAR;
-  auto b_work_full = [&](int i) { return bar0 + 8 * i; };
-  auto b_work_empty = [&](int i) { return bar0 + 16 + 8 * i; };
-  auto b_q_full = [&](int i) { return bar0 + 32 + 8 * i; };
-  auto b_q_empty = [&](int i) { return bar0 + 48 + 8 * i; };
-  auto b_s_full = [&](int i) { return bar0 + 64 + 8 * i; };
-  auto b_p_ready = [&](int i) { return bar0 + 80 + 8 * i; };
-  auto b_pv_done = [&](int i) { return bar0 + 96 + 8 * i; };
-  auto b_o_full = [&](int i) { return bar0 + 112 + 8 * i; };
-  auto b_o_empty = [&](int i) { return bar0 + 128 + 8 * i; };
-  auto b_p_half = [&](int i) { return bar0 + 144 + 8 * i; };
-  const uint32_t bar1 = bar0 + 160;
+  auto b_q_full = [&](int i) { return bar0 + 8 * i; };
+  auto b_q_empty = [&](int i) { return bar0 + 16 + 8 * i; };
+  auto b_s_full = [&](int i) { return bar0 + 32 + 8 * i; };
+  auto b_p_half = [&](int i) { return bar0 + 48 + 8 * i; };
+  auto b_p_ready = [&](int i) { return bar0 + 64 + 8 * i; };
+  auto b_pv_done = [&](int i) { return bar0 + 80 + 8 * i; };
+  auto b_o_full = [&](int i) { return bar0 + 96 + 8 * i; };
+  auto b_o_empty = [&](int i) { return bar0 + 112 + 8 * i; };
+  auto b_work_full = [&](int n) { return bar0 + 128 + 8 * (n % kWtRing); };
+  auto b_work_empty = [&](int n) { return bar0 + 128 + 8 * (kWtRing + n % kWtRing); };
+  const uint32_t bar1 = bar0 + 128 + 16 * kWtRing;
   auto b_k_full = [&](int s) { return bar1 + 8 * s; };
   auto b_k_empty = [&](int s) { return bar1 + 8 * (C::NK + s); };
   auto b_v_full = [&](int s) { return bar1 + 8 * (2 * C::NK + s); };
@@ -141,8 +191,6 @@ window_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
 
   if (tid == 0) {
     for (int i = 0; i < 2; ++i) {
-      mbar_init(b_work_full(i), 1);
-      mbar_init(b_work_empty(i), 11);
       mbar_init(b_q_full(i), 1);
       mbar_init(b_q_empty(i), 1);
       mbar_init(b_s_full(i), 1);
@@ -152,6 +200,7 @@ window_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
       mbar_init(b_o_full(i), 1);
       mbar_init(b_o_empty(i), 4);
     }
+    for (int i = 0; i < kWtRing; ++i) { mbar_init(b_work_full(i), 1); mbar_init(b_work_empty(i), 11); }
     for (int s = 0; s < C::NK; ++s) { mbar_init(b_k_full(s), 1); mbar_init(b_k_empty(s), 1); }
     for (int s = 0; s < C::NV; ++s) { mbar_init(b_v_full(s), 1); mbar_init(b_v_ready(s), 1); mbar_init(b_v_empty(s), 1); }
     *abort_flag = 0;
@@ -171,7 +220,7 @@ window_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
   auto wait = [&](uint32_t bar, uint32_t phase) { return mbar_wait(bar, phase & 1, abort_flag, prm.w.status, prm.wait_limit); };
   auto relaxed = [&](uint32_t bar, uint32_t phase) { return mbar_wait_relaxed(bar, phase & 1, abort_flag, prm.w.status, prm.wait_limit); };
   auto read_work = [&](int n, Work& w) {               // a thread's copy of piece n, which is there
-    const volatile int* src = reinterpret_cast<const volatile int*>(work_ring + (n & 1));
+    const volatile int* src = reinterpret_cast<const volatile int*>(work_ring + n % kWtRing);
     int* dst = reinterpret_cast<int*>(&w);
 #pragma unroll
     for (int i = 0; i < 12; ++i) dst[i] = src[i];
@@ -180,20 +229,31 @@ window_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
   if (warp == 3) {
     // ---------------------------------------------------------- work
     if (lane == 0) {
+      const int all_blocks = prm.w.pieces[prm.w.batch], n_work = all_blocks * prm.w.heads_q;
       int n = 0;
-      for (int idx = blockIdx.x;;) {
+      for (int idx = blockIdx.x;; ++n) {
         Work w;
         w.b = -1;
-        if (idx < prm.n_work) {
-          const int rb = idx % prm.blocks, bh = idx / prm.blocks;
-          w.b = bh / prm.w.heads_q;
-          w.h = bh % prm.w.heads_q;
-          w.r0 = rb * kWtRows;
+        if (idx < n_work) {
+          // the blocks of a head one after the other, or the last blocks of all heads first
+          int block = idx % all_blocks;
+          w.h = idx / all_blocks;
+          if (prm.rows_first) {
+            w.h = idx % prm.w.heads_q;
+            block = all_blocks - 1 - idx / prm.w.heads_q;
+          }
+          idx = (int)gridDim.x + atomicAdd(prm.w.status + kNextWord, 1);
+          int lo = 0, hi = prm.w.batch - 1;            // the batch item of the block
+          while (lo < hi) {
+            const int mid = (lo + hi + 1) >> 1;
+            if (prm.w.pieces[mid] <= block) lo = mid;
+            else hi = mid - 1;
+          }
+          w.b = lo;
+          w.r0 = (block - prm.w.pieces[lo]) * kWtRows;
           const WindowItem it(prm.w, w.b);
           w.len_q = it.len_q;
           w.len_k = it.len_k;
-          idx = (int)gridDim.x + atomicAdd(prm.next, 1);
-          if (w.r0 >= it.len_q) continue;
           const WindowSpan all(prm.w, it, w.r0, min(w.r0 + kWtRows, it.len_q), kWtKeys);
           w.tiles = all.tiles;
           w.sink_tiles = all.sink_tiles;
@@ -209,13 +269,12 @@ window_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
             }
           }
         }
-        if (n >= 2 && !relaxed(b_work_empty(n & 1), (n >> 1) - 1)) break;
-        volatile int* dst = reinterpret_cast<volatile int*>(work_ring + (n & 1));
+        if (n >= kWtRing && !relaxed(b_work_empty(n), n / kWtRing - 1)) break;
+        volatile int* dst = reinterpret_cast<volatile int*>(work_ring + n % kWtRing);
         const int* src = reinterpret_cast<const int*>(&w);
 #pragma unroll
         for (int i = 0; i < 12; ++i) dst[i] = src[i];
-        mbar_arrive(b_work_full(n & 1));
-        ++n;
+        mbar_arrive(b_work_full(n));
         if (w.b < 0) break;
       }
     }
@@ -229,28 +288,28 @@ window_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
       uint32_t k_ph = 1, v_ph = 1;
       bool ok = true;
       for (int n = 0; ok; ++n) {
-        if (!relaxed(b_work_full(n & 1), n >> 1)) break;
+        if (!relaxed(b_work_full(n), n / kWtRing)) break;
         Work w;
         read_work(n, w);
-        mbar_arrive(b_work_empty(n & 1));
+        mbar_arrive(b_work_empty(n));
         if (w.b < 0) break;
         const int g = w.h / prm.w.group;
         bool q_there[2] = {false, false};
         for (int u = 0; u < w.tiles && ok; ++u) {
           const int t = w.tile(u);
+          // queries of the tiles that begin here: the first before the keys, which wait for less than the second
+          auto queries = [&](int i) {
+            if (q_there[i] || !w.active(i, t, sinks)) return;
+            q_there[i] = true;
+            if (q_used[i] > 0) ok = ok && relaxed(b_q_empty(i), q_used[i] - 1);
+            if (!ok) return;
+            ++q_used[i];
+            mbar_expect_tx(b_q_full(i), C::TILE_BYTES);
 #pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            if (!q_there[i] && w.active(i, t, sinks)) {
-              q_there[i] = true;
-              if (q_used[i] > 0) ok = ok && relaxed(b_q_empty(i), q_used[i] - 1);
-              if (!ok) break;
-              ++q_used[i];
-              mbar_expect_tx(b_q_full(i), C::TILE_BYTES);
-#pragma unroll
-              for (int pn = 0; pn < C::PANELS; ++pn)
-                tma_load_4d(s_q + i * C::TILE_BYTES + pn * C::PANEL_BYTES, &tm_q, pn * 64, w.r0 + i * kWindowTile, w.h, w.b, b_q_full(i));
-            }
-          }
+            for (int pn = 0; pn < C::PANELS; ++pn)
+              tma_load_4d(s_q + i * C::TILE_BYTES + pn * C::PANEL_BYTES, &tm_q, pn * 64, w.r0 + i * kWindowTile, w.h, w.b, b_q_full(i));
+          };
+          queries(0);
           if (!ok) break;
           if (steps >= C::NK && !relaxed(b_k_empty(k_slot), k_ph)) { ok = false; break; }
           mbar_expect_tx(b_k_full(k_slot), C::TILE_BYTES);
@@ -258,6 +317,8 @@ window_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
           for (int pn = 0; pn < C::PANELS; ++pn)
             tma_load_4d(s_k + k_slot * C::TILE_BYTES + pn * C::PANEL_BYTES, &tm_k, pn * 64, t * kWtKeys, g, w.b, b_k_full(k_slot));
           if (++k_slot == C::NK) { k_slot = 0; k_ph ^= 1; }
+          queries(1);
+          if (!ok) break;
           if (steps >= C::NV && !relaxed(b_v_empty(v_slot), v_ph)) { ok = false; break; }
           mbar_expect_tx(b_v_full(v_slot), C::TILE_BYTES);
 #pragma unroll
@@ -274,12 +335,12 @@ window_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
     uint32_t ph = 0;
     bool ok = true;
     for (int n = 0; ok; ++n) {
-      ok = __all_sync(0xffffffffu, relaxed(b_work_full(n & 1), n >> 1));
+      ok = __all_sync(0xffffffffu, relaxed(b_work_full(n), n / kWtRing));
       if (!ok) break;
       Work w;
       read_work(n, w);
       __syncwarp();
-      if (lane == 0) mbar_arrive(b_work_empty(n & 1));
+      if (lane == 0) mbar_arrive(b_work_empty(n));
       if (w.b < 0) break;
       for (int u = 0; u < w.tiles; ++u) {
         ok = __all_sync(0xffffffffu, relaxed(b_v_full(slot), ph));
@@ -320,9 +381,9 @@ window_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
       while (ok) {
         // the step that comes: the next key tile of this piece of work or the first one of the next
         while (more && u >= w.tiles) {
-          if (!wait(b_work_full(n & 1), n >> 1)) { ok = false; break; }
+          if (!wait(b_work_full(n), n / kWtRing)) { ok = false; break; }
           read_work(n, w);
-          mbar_arrive(b_work_empty(n & 1));
+          mbar_arrive(b_work_empty(n));
           ++n;
           u = 0;
           begun[0] = begun[1] = false;
@@ -340,14 +401,23 @@ window_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
         }
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
+          // A look at a barrier takes some 200 cycles, done or not: all that is there early (loads, a free accumulator) is looked
+          // at before P, whose softmax it overlaps with.
+          if (i == 0) {
+            if (any_before && !wait(b_v_ready(v_slot), v_ph)) { ok = false; break; }
+            if (more && !wait(b_k_full(k_slot), k_ph)) { ok = false; break; }
+          }
+          if (first[i]) {
+            if (!wait(b_q_full(i), n_q[i])) { ok = false; break; }
+            ++n_q[i];
+          }
           if (on[i]) {
             // O of query tile i += P V of the step before
-            if (!wait(b_p_half(i), n_pv[i])) { ok = false; break; }
-            if (!wait(b_v_ready(v_slot), v_ph)) { ok = false; break; }
             if (was_first[i]) {
               if (n_o[i] > 0 && !wait(b_o_empty(i), n_o[i] - 1)) { ok = false; break; }
               ++n_o[i];
             }
+            if (!wait(b_p_half(i), n_pv[i])) { ok = false; break; }
             tc_fence_after();
             const uint64_t vd = v_desc0 + ((v_slot * C::TILE_BYTES) >> 4);
 #pragma unroll
@@ -358,22 +428,15 @@ window_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
 #pragma unroll
             for (int ks = 4; ks < 8; ++ks)
               mma_ts(tmem_o(i), tmem_s(i) + ks * 8, vd + (uint64_t)(ks * (2048 >> 4)), idesc_pv, 1u);
-            mma_commit(b_pv_done(i));
-            if (was_last[i]) mma_commit(b_o_full(i));
             ++n_pv[i];
           }
-          if (i == 1 && any_before) {
-            mma_commit(b_v_empty(v_slot));
-            if (++v_slot == C::NV) { v_slot = 0; v_ph ^= 1; }
-          }
           if (now[i]) {
-            if (first[i]) {
-              if (!wait(b_q_full(i), n_q[i])) { ok = false; break; }
-              ++n_q[i];
-            }
-            if (!wait(b_k_full(k_slot), k_ph)) { ok = false; break; }
             tc_fence_after();
             const uint64_t qd = q_desc0 + ((i * C::TILE_BYTES) >> 4), kd = k_desc0 + ((k_slot * C::TILE_BYTES) >> 4);
+            if (on[i]) {                                     // (commits behind the products of both: nothing waits for O alone unless the tile ends)
+              mma_commit(b_pv_done(i));
+              if (was_last[i]) mma_commit(b_o_full(i));
+            }
 #pragma unroll
             for (int ks = 0; ks < D / 16; ++ks) {
               const uint32_t off = ((ks / 4) * C::PANEL_BYTES + (ks % 4) * 32) >> 4;
@@ -382,6 +445,13 @@ window_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
             mma_commit(b_s_full(i));
             if (last[i]) mma_commit(b_q_empty(i));
             ++n_s[i];
+          } else if (on[i]) {
+            mma_commit(b_pv_done(i));
+            if (was_last[i]) mma_commit(b_o_full(i));
+          }
+          if (i == 1 && any_before) {
+            mma_commit(b_v_empty(v_slot));
+            if (++v_slot == C::NV) { v_slot = 0; v_ph ^= 1; }
           }
         }
         if (!ok) break;
@@ -407,80 +477,69 @@ window_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
     int steps = 0, results = 0;
     bool ok = true;
     for (int n = 0; ok; ++n) {
-      ok = all_wait(b_work_full(n & 1), n >> 1);
+      ok = all_wait(b_work_full(n), n / kWtRing);
       if (!ok) break;
-      Work w;
-      read_work(n, w);
-      __syncwarp();
-      if (lane == 0) mbar_arrive(b_work_empty(n & 1));
+      const volatile Work& w = work_ring[n % kWtRing];       // (read where it is needed: registers are few)
       if (w.b < 0) break;
       const int r = w.r0 + i * kWindowTile + row;            // query row
-      if (w.r0 + i * kWindowTile >= w.len_q) continue;
+      if (w.r0 + i * kWindowTile >= w.len_q) {
+        __syncwarp();
+        if (lane == 0) mbar_arrive(b_work_empty(n));
+        continue;
+      }
       const WindowItem it(w.len_q, w.len_k);
-      const WindowSpan span(prm.w, it, w.r0 + i * kWindowTile, min(w.r0 + (i + 1) * kWindowTile, w.len_q), kWtKeys);
+      const WindowSpan span(prm.w, it, w.r0 + i * kWindowTile, min(w.r0 + (i + 1) * kWindowTile, it.len_q), kWtKeys);
       const WindowRow sees(prm.w, it, r);
-      const int lo = i == 0 ? w.lo[0] : w.lo[1], hi = i == 0 ? w.hi[0] : w.hi[1];
-      float m = -INFINITY, l = 0.f;
+      float m = r < it.len_q ? -INFINITY : 0.f, l = 0.f, pend = 0.f;      // (a row behind the last one needs no reference)
       bool begun = false;
 #pragma unroll 1
       for (int u = 0; u < w.tiles; ++u) {
-        const int t = w.tile(u), j0 = t * kWtKeys;
-        if (!Work::takes_part(lo, hi, t, sinks)) continue;
+        const int j0 = (u < w.sink_tiles ? u : w.tile_lo + u - w.sink_tiles) * kWtKeys;
+        if (!Work::takes_part(span.lo, span.hi, j0, sinks)) continue;
         ok = all_wait(b_s_full(i), steps);
         if (!ok) break;
         tc_fence_after();
-        float top = -INFINITY;
+        const bool masked = !span.whole(j0, j0 + kWtKeys);
         uint32_t sa[32], sb[32];
-        auto maximum = [&](const uint32_t (&s)[32]) {
-          float x0 = -INFINITY, x1 = -INFINITY;
-#pragma unroll
-          for (int e = 0; e < 32; e += 4) {
-            x0 = max3(x0, __uint_as_float(s[e]), __uint_as_float(s[e + 1]));
-            x1 = max3(x1, __uint_as_float(s[e + 2]), __uint_as_float(s[e + 3]));
-          }
-          top = max3(top, x0, x1);
-        };
-        if (span.whole(j0, j0 + kWtKeys)) {
-          tmem_ld32(t_s, sa);
-          tmem_ld32(t_s + 32, sb);
-          tmem_wait_ld32(sa);
-          maximum(sa);
-          tmem_wait_ld32(sb);
-          tmem_ld32(t_s + 64, sa);
-          maximum(sb);
-          tmem_ld32(t_s + 96, sb);
-          tmem_wait_ld32(sa);
-          maximum(sa);
-          tmem_wait_ld32(sb);
-          maximum(sb);
-        } else {
-          const int end = sees.end - j0, from = sees.from - j0, sink = sinks - j0;
-#pragma unroll 1
-          for (int c = 0; c < 128; c += 32) {
-            tmem_ld32(t_s + c, sa);
-            auto below = [&](int x) {
-              const int k = x - c;
-              return k >= 32 ? 0xffffffffu : k <= 0 ? 0u : (1u << k) - 1u;
-            };
-            const unsigned seen = below(end) & (~below(from) | below(sink));
-            tmem_wait_ld32(sa);
-#pragma unroll
-            for (int e = 0; e < 32; ++e)
-              if (!((seen >> e) & 1u)) sa[e] = 0xff800000u;
-            tmem_st32(t_s + c, sa);
-            maximum(sa);
-          }
-          tmem_wait_st();
-        }
         tmem_ld32(t_s, sa);
-        top *= scale;
-        const bool raise = top > m + kWtRaise || (m == -INFINITY && top > -INFINITY);
-        if (__any_sync(0xffffffffu, raise)) {
-          const float up = raise ? top : m;
+        // what a row does not see of columns c .. c + 31: columns at or behind `end`, and those before `from` that are no first tokens
+        auto mask = [&](uint32_t (&s)[32], int c) {
+          auto below = [&](int x) {                          // bits of columns below x
+            const int k = x - j0 - c;
+            return k >= 32 ? 0xffffffffu : k <= 0 ? 0u : (1u << k) - 1u;
+          };
+          const unsigned seen = below(sees.end) & (~below(sees.from) | below(sinks));
+#pragma unroll
+          for (int e = 0; e < 32; ++e)
+            if (!((seen >> e) & 1u)) s[e] = 0xff800000u;
+        };
+        // ---- reference
+        if (__any_sync(0xffffffffu, m == -INFINITY || pend > 0.f)) {
+          float up = m + pend;
+          if (__any_sync(0xffffffffu, m == -INFINITY)) {
+            float top = -INFINITY;
+#pragma unroll 1
+            for (int c = 0; c < kWtKeys; c += 32) {
+              tmem_ld32(t_s + c, sa);
+              tmem_wait_ld32(sa);
+              if (masked) mask(sa, c);
+              float x0 = -INFINITY, x1 = -INFINITY;
+#pragma unroll
+              for (int e = 0; e < 32; e += 4) {
+                x0 = max3(x0, __uint_as_float(sa[e]), __uint_as_float(sa[e + 1]));
+                x1 = max3(x1, __uint_as_float(sa[e + 2]), __uint_as_float(sa[e + 3]));
+              }
+              top = max3(top, x0, x1);
+            }
+            if (m == -INFINITY) up = top * scale;
+            tmem_ld32(t_s, sa);
+          }
           const float by = m == -INFINITY ? 0.f : ex2_approx(m - up);
           l *= by;
           m = up;
+          pend = 0.f;
           if (begun) {
+            // the products of the step before are complete; those of this step wait for this warp
             ok = all_wait(b_pv_done(i), steps - 1);
             if (!ok) break;
             tc_fence_after();
@@ -495,11 +554,14 @@ window_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
             }
           }
         }
+        // ---- probabilities: column c to half a word
         const float ref = m == -INFINITY ? 0.f : -m;
         const f32x2 sc2 = pack2(scale, scale), nm2 = pack2(ref, ref);
-        f32x2 sum0 = pack2(0.f, 0.f), sum1 = sum0;
-        auto exponentials = [&](const uint32_t (&s)[32], uint32_t dst) {
+        float big = 0.f;                                     // largest sum of 32
+        auto exponentials = [&](uint32_t (&s)[32], int c) {
+          if (masked) mask(s, c);
           uint32_t pk[16];
+          f32x2 sum0 = pack2(0.f, 0.f), sum1 = sum0;
 #pragma unroll
           for (int e = 0; e < 32; e += 4) {
             f32x2 x01 = fma2(pack2(__uint_as_float(s[e]), __uint_as_float(s[e + 1])), sc2, nm2);
@@ -514,70 +576,82 @@ window_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
             pk[e / 2] = pack_bf16x2(x0, x1);
             pk[e / 2 + 1] = pack_bf16x2(x2, x3);
           }
-          tmem_st16(dst, pk);
+          float a0, a1, a2, a3;
+          unpack2(sum0, a0, a1);
+          unpack2(sum1, a2, a3);
+          const float sum = (a0 + a1) + (a2 + a3);
+          l += sum;
+          big = fmaxf(big, sum);
+          tmem_st16(t_s + c / 2, pk);
         };
         tmem_wait_ld32(sa);
         tmem_ld32(t_s + 32, sb);
-        exponentials(sa, t_s);
+        exponentials(sa, 0);
         tmem_wait_ld32(sb);
         tmem_ld32(t_s + 64, sa);
-        exponentials(sb, t_s + 16);
+        exponentials(sb, 32);
         tmem_wait_st();
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(b_p_half(i));
+        if (lane == 0) mbar_arrive(b_p_half(i));             // the products of the first 64 keys need not wait for the others
         tmem_wait_ld32(sa);
         tmem_ld32(t_s + 96, sb);
-        exponentials(sa, t_s + 32);
+        exponentials(sa, 64);
         tmem_wait_ld32(sb);
-        exponentials(sb, t_s + 48);
+        exponentials(sb, 96);
         tmem_wait_st();
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(b_p_ready(i));
-        float a0, a1, a2, a3;
-        unpack2(sum0, a0, a1);
-        unpack2(sum1, a2, a3);
-        l += (a0 + a1) + (a2 + a3);
+        if (big > kWtSumLimit) pend = ceilf(log2f(big));
         begun = true;
         ++steps;
       }
       if (!ok) break;
       // ---- O / l; a row that sees nothing: zeros, log-sum-exp -inf
-      const bool live = r < w.len_q, empty = l < 0.5f;
+      const bool live = r < it.len_q, empty = l == 0.f;
       const float inv = empty ? 0.f : 1.f / l;
       __nv_bfloat16* out = static_cast<__nv_bfloat16*>(prm.w.o) + w.b * prm.w.o_b + w.h * prm.w.o_h + r * prm.w.o_n;
-      float any = 0.f;
       if (begun) {
         ok = all_wait(b_o_full(i), results);
         if (!ok) break;
         ++results;
         tc_fence_after();
       }
+      f32x2 any2 = pack2(0.f, 0.f);
+      uint32_t o[32];
 #pragma unroll 1
-      for (int c = 0; c < D / 32; ++c) {
-        uint32_t o[32];
-#pragma unroll
-        for (int e = 0; e < 32; ++e) o[e] = 0u;
+      for (int c = 0; c < D; c += 32) {
         if (begun) {
-          tmem_ld32(t_o + c * 32, o);
+          tmem_ld32(t_o + c, o);
           tmem_wait_ld32(o);
         }
+        uint32_t x[16];
 #pragma unroll
-        for (int e = 0; e < 32; ++e) any += __uint_as_float(o[e]);
+        for (int e = 0; e < 16; ++e) {
+          const f32x2 y = mul2(pack2(__uint_as_float(o[2 * e]), __uint_as_float(o[2 * e + 1])), pack2(inv, inv));
+          any2 = add2(any2, y);
+          float y0, y1;
+          unpack2(y, y0, y1);
+          x[e] = empty ? 0u : pack_bf16x2(y0, y1);
+        }
         if (live) {
-          uint4* dst = reinterpret_cast<uint4*>(out + c * 32);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            uint4 x;
-            x.x = pack_bf16x2(__uint_as_float(o[8 * e + 0]) * inv, __uint_as_float(o[8 * e + 1]) * inv);
-            x.y = pack_bf16x2(__uint_as_float(o[8 * e + 2]) * inv, __uint_as_float(o[8 * e + 3]) * inv);
-            x.z = pack_bf16x2(__uint_as_float(o[8 * e + 4]) * inv, __uint_as_float(o[8 * e + 5]) * inv);
-            x.w = pack_bf16x2(__uint_as_float(o[8 * e + 6]) * inv, __uint_as_float(o[8 * e + 7]) * inv);
-            dst[e] = empty ? make_uint4(0u, 0u, 0u, 0u) : x;
+          for (int e = 0; e < 16; e += 8) {
+            __nv_bfloat16* dst = out + c + 2 * e;
+            if (prm.wide) {                                  // whole sectors at a time
+              asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(dst), "r"(x[e]), "r"(x[e + 1]), "r"(x[e + 2]),
+                           "r"(x[e + 3]), "r"(x[e + 4]), "r"(x[e + 5]), "r"(x[e + 6]), "r"(x[e + 7]) : "memory");
+            } else {
+              reinterpret_cast<uint4*>(dst)[0] = make_uint4(x[e], x[e + 1], x[e + 2], x[e + 3]);
+              reinterpret_cast<uint4*>(dst)[1] = make_uint4(x[e + 4], x[e + 5], x[e + 6], x[e + 7]);
+            }
           }
         }
       }
+      float any, any_odd;
+      unpack2(any2, any, any_odd);
+      any += any_odd;
       if (begun) {
         tc_fence_before();
         __syncwarp();
@@ -588,8 +662,9 @@ window_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
       // rows to be computed again: a word for each 32
       const bool again = __any_sync(0xffffffffu, live && !empty && !(fabsf(any) < INFINITY && l < INFINITY));
       if (lane == 0) {
-        prm.w.redo[((size_t)(w.b * prm.w.heads_q + w.h) * prm.blocks + w.r0 / kWtRows) * 16 + (i * 4 + quarter) * 2] = prm.w.redo[((size_t)(w.b * prm.w.heads_q + w.h) * prm.blocks + w.r0 / kWtRows) * 16 + (i * 4 + quarter) * 2 + 1] = again ? 1 : 0;
-        if (again) atomicExch(prm.w.redo_any, 1);
+        prm.w.redo[((size_t)(w.b * prm.w.heads_q + w.h) * prm.blocks + w.r0 / kWtRows) * 8 + i * 4 + quarter] = again ? 1 : 0;
+        if (again) atomicExch(prm.w.status + kRedoWord, 1);
+        mbar_arrive(b_work_empty(n));
       }
     }
   }
@@ -631,19 +706,19 @@ static bool rows_map(CUtensorMap* map, const void* base, int D, int n, int heads
 }
 
 template <int D>
-static int launch_window_tc_d(const CUtensorMap* maps, const WtParams& prm, LaunchStream st) {
+static int launch_window_tc_d(const CUtensorMap* maps, const WtParams& prm, int n_work, LaunchStream st) {
   auto kernel = window_tc_kernel<D>;
   int dev = 0, sms = 0;
   CA_RETURN_IF_CUDA(cudaGetDevice(&dev));
   CA_RETURN_IF_CUDA(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
   CA_RETURN_IF_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, WtCfg<D>::SMEM));
-  launch_chained(kernel, prm.n_work < sms ? prm.n_work : sms, kWtThreads, WtCfg<D>::SMEM, st, maps[0], maps[1], maps[2], prm);
+  launch_chained(kernel, n_work < sms ? n_work : sms, kWtThreads, WtCfg<D>::SMEM, st, maps[0], maps[1], maps[2], prm);
   CA_LAUNCH_CHECK();
   return CA_OK;
 }
 
 // CA_ERR_UNSUPPORTED: strides that a tensor map does not describe
-int launch_window_tc(const WindowParams& w, int D, int* next, LaunchStream st) {
+int launch_window_tc(const WindowParams& w, int D, LaunchStream st) {
   CUtensorMap maps[3];
   if (!rows_map(&maps[0], w.q, D, w.n_q, w.heads_q, w.batch, w.q_n, w.q_h, w.q_b) ||
       !rows_map(&maps[1], w.k, D, w.n_k, w.heads_kv, w.batch, w.k_n, w.k_h, w.k_b) ||
@@ -651,13 +726,20 @@ int launch_window_tc(const WindowParams& w, int D, int* next, LaunchStream st) {
     return CA_ERR_UNSUPPORTED;
   WtParams prm{};
   prm.w = w;
-  prm.next = next;
   prm.blocks = ceil_div(w.n_q, kWtRows);
-  if ((long long)prm.blocks * w.heads_q * w.batch > 0x3fffffffLL) return CA_ERR_UNSUPPORTED;
-  prm.n_work = prm.blocks * w.heads_q * w.batch;
+  const long long n_work = (long long)prm.blocks * w.heads_q * w.batch;
+  if (n_work > 0x3fffffffLL) return CA_ERR_UNSUPPORTED;
+  // Pieces are handed out head by head, whose blocks read the same keys; or, where the keys and values that all heads' windows
+  // reach at a time stay in L2 (126 MB; two thirds of it), last blocks of all heads first, so that the short ones at the start of a
+  // causal sequence even out the end of the call.
+  const double reach = (w.left < 0 ? w.n_k : fmin((double)w.n_k, (double)w.left + (w.right < 0 ? w.n_k : w.right) + 2.0 * kWtRows));
+  prm.rows_first = (double)w.batch * w.heads_kv * reach * D * 4 < 80e6;
   prm.wait_limit = kWaitLimitCycles;
-  CA_RETURN_IF_CUDA(cudaMemsetAsync(w.status, 0, kStatusBytes, st));
-  return D == 64 ? launch_window_tc_d<64>(maps, prm, st) : launch_window_tc_d<128>(maps, prm, st);
+  prm.wide = (reinterpret_cast<uintptr_t>(w.o) % 32 == 0) && (w.batch == 1 || w.o_b % 16 == 0) && (w.heads_q == 1 || w.o_h % 16 == 0) &&
+             (w.n_q == 1 || w.o_n % 16 == 0);
+  launch_chained(window_prepare_kernel, 1, 256, 0, st, w);
+  CA_LAUNCH_CHECK();
+  return D == 64 ? launch_window_tc_d<64>(maps, prm, (int)n_work, st) : launch_window_tc_d<128>(maps, prm, (int)n_work, st);
 }
 
 }  // namespace ca
