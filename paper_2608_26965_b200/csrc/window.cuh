@@ -12,7 +12,7 @@ struct WindowParams {
   const int32_t *len_q, *len_k;     // [batch] or null
   int* status;
   int32_t* pieces;                  // [batch + 1] blocks of kWindowBlock rows of the batch items before
-  int32_t* redo;                    // [batch * heads_q][blocks of kWindowBlock rows][8]: 32 rows each, to be computed again (null: all)
+  int32_t* redo;                    // [batch * heads_q][blocks of kWindowBlock rows][16]: 16 rows each, to be computed again (null: all)
   int batch, heads_q, heads_kv, group, n_q, n_k, left, right, sinks;
   float scale_log2;
 };
@@ -67,6 +67,9 @@ struct WindowRow {
   __device__ __forceinline__ bool sees(int j) const { return j < end && (j >= from || j < sinks); }
 };
 
+// The tensor-core kernel wants window_prepare before it (pieces, counters and status), and window_ref behind it, with `redo` set, for
+// the rows that it marked.
+int launch_window_prepare(const WindowParams& prm, LaunchStream st);
 int launch_window_ref(const WindowParams& prm, int D, int dtype, LaunchStream st);
 int launch_window_tc(const WindowParams& prm, int D, LaunchStream st);    // CA_ERR_UNSUPPORTED: strides that it does not take
 

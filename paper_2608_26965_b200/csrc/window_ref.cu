@@ -1,186 +1,245 @@
 // Attention over a sliding window on the CUDA cores, in fp32: fp32 storage, and the rows that the tensor-core kernel
 // leaves to it.
-//     S = Q K^T, P = exp2(s c - m) over the visible keys, O = P V / sum P,    m the running maximum of a row.
-// A CTA takes 64 query rows and goes over the keys that they see, 64 at a time; a thread has 4 x 4 scores and 4 x D/16
-// columns of the result in registers, so that shared memory is read 8 times (P V: 4 + D/16) for 64 (D) multiply-adds.
+//     S = Q K^T, P = exp2(S c - m) over the visible keys, O = P V / sum P,    m the running maximum of a row.
+// A CTA takes M query rows and goes over the keys that they see, 32 at a time, which arrive while the 32 before are worked on (fp32
+// storage).  A thread has R x 4 scores and R x D/8 columns of the result in registers.  What bounds it is reading shared memory, not the
+// multiply-adds (two to an instruction): a vector of 16 bytes per lane takes the 3.6 cycles of four whether lanes read the same
+// one or not, so 8 vectors for 32 instructions (R = 4) keep the reads of four warps at it for 115 cycles and the multiply-adds
+// for 64.  2 x 8 heads of 4,000 rows, causal, d = 128: 2.08 ms, 31 TFLOP/s of visible pairs (R = 2 2.93 ms; R = 8 3.19, for want of
+// registers and warps).  12 heads of 1,370 rows, d = 64, 148 rows to either side: 73 us.  M = 64 with R = 4; M = 32 with R = 2 where
+// tiles of 64 rows would be fewer than one to an SM (100 rows, one head: 10.4 us instead of 15.4).
+// (Products of tf32 halves on the tensor cores, three for one, took 56 us for the 1,370 rows, but their sums are cut instead of rounded:
+// 2.7e-6 off where this kernel and a plain one are 6.4e-7.)
 // Only tiles at a border of the window are masked: what a row does not see takes no part, whatever stands there
 // (0 x infinity would).
 #include <math.h>
+
+#include <type_traits>
 
 #include "tc_ptx.cuh"
 #include "window.cuh"
 
 namespace ca {
 
-constexpr int kWrRows = 64, kWrKeys = 64, kWrThreads = 256;
+using namespace ptx;
 
-template <typename T, int D>
-__device__ __forceinline__ void window_rows_to_smem(float* dst, const T* src, long long stride, int rows, int tid) {
+constexpr int kWrKeys = 32;
+
+template <int D, int M>
+struct WrCfg {
+  static constexpr int R = M == 32 ? 2 : 4;           // query rows of a thread
+  static constexpr int THREADS = M / R * 8;
+  static constexpr int PITCH = D + 4;           // floats: rows a vector apart from a multiple of the banks
+  static constexpr int P_PITCH = kWrKeys + 4;
+  static constexpr int KV = kWrKeys * PITCH;    // a tile of keys, of values
+  static constexpr int OFF_KV = M * PITCH, OFF_P = OFF_KV + 4 * KV;
+  static constexpr int SMEM = (OFF_P + M * P_PITCH) * 4;
+};
+
+// rows of [.., D] into shared memory as fp32; rows from `there` on as zeros
+template <typename T, int D, int THREADS, int ROWS>
+__device__ __forceinline__ void window_rows_to_smem(float* dst, const T* src, long long stride, int there, int tid) {
   constexpr int V = D / 4;
-#pragma unroll 4
-  for (int i = tid; i < 64 * V; i += kWrThreads) {
+#pragma unroll
+  for (int i = tid; i < ROWS * V; i += THREADS) {
     const int r = i / V, c = i % V * 4;
-    const float4 x = r < rows ? load4(src + r * stride + c) : make_float4(0.f, 0.f, 0.f, 0.f);
-    *reinterpret_cast<float4*>(dst + r * (D + 4) + c) = x;
+    float* to = dst + r * (D + 4) + c;
+    if constexpr (std::is_same<T, float>::value) {
+      const int bytes = r < there ? 16 : 0;
+      asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(to)), "l"(src + (r < there ? r * stride + c : 0)), "r"(bytes) : "memory");
+    } else {
+      *reinterpret_cast<float4*>(to) = r < there ? load4(src + r * stride + c) : make_float4(0.f, 0.f, 0.f, 0.f);
+    }
   }
 }
 
-template <typename T, int D>
-__global__ void __launch_bounds__(kWrThreads) window_ref_kernel(const __grid_constant__ WindowParams prm) {
+template <typename T, int D, int M>
+__global__ void __launch_bounds__(WrCfg<D, M>::THREADS) window_ref_kernel(const __grid_constant__ WindowParams prm) {
   wait_for_previous();
   let_next_start();
+  using C = WrCfg<D, M>;
+  constexpr int R = C::R;
   extern __shared__ __align__(16) float smf[];
-  float* sq = smf;                              // [64][D + 4]: rows a vector apart from a multiple of the banks
-  float* sk = sq + kWrRows * (D + 4);
-  float* sv = sk + kWrKeys * (D + 4);
-  float* sp = sv + kWrKeys * (D + 4);           // [64][68]
-  const int tid = threadIdx.x, ty = tid >> 4, tx = tid & 15;
+  float* sq = smf;
+  float* sp = smf + C::OFF_P;
+  const int tid = threadIdx.x, ty = tid >> 3, tx = tid & 7;
   if (prm.redo) {
     if (prm.status[kRedoWord] == 0) return;
   } else if (blockIdx.x == 0) {
     // the only one that writes the status word
     int bad = 0;
-    for (int i = tid; i < prm.batch; i += kWrThreads)
+    for (int i = tid; i < prm.batch; i += C::THREADS)
       bad |= (prm.len_q && (unsigned)prm.len_q[i] > (unsigned)prm.n_q) || (prm.len_k && (unsigned)prm.len_k[i] > (unsigned)prm.n_k);
     bad = __syncthreads_or(bad);
     if (tid == 0) *prm.status = bad ? CA_ERR_BAD_INDEX : CA_OK;
   }
-  const int blocks64 = (prm.n_q + kWrRows - 1) / kWrRows;
-  const long long n_work = (long long)blocks64 * prm.heads_q * prm.batch;
+  const int blocks = (prm.n_q + M - 1) / M;
+  const long long n_work = (long long)blocks * prm.heads_q * prm.batch;
 #pragma unroll 1
   for (long long idx = blockIdx.x; idx < n_work; idx += gridDim.x) {
-  const int r0 = (int)(idx % blocks64) * kWrRows, bh = (int)(idx / blocks64), b = bh / prm.heads_q, h = bh % prm.heads_q;
-  const WindowItem it(prm, b);
-  if (r0 >= it.len_q) continue;
-  if (prm.redo) {
-    const int32_t* marks = prm.redo + ((size_t)bh * ((prm.n_q + kWindowBlock - 1) / kWindowBlock) + r0 / kWindowBlock) * 8 + r0 % kWindowBlock / 32;
-    if ((marks[0] | marks[1]) == 0) continue;
-  }
-  const int rows = min(kWrRows, it.len_q - r0);
-  const WindowSpan span(prm, it, r0, r0 + rows, kWrKeys);
-  const int g = h / prm.group;
-  const T* q = static_cast<const T*>(prm.q) + b * prm.q_b + h * prm.q_h + r0 * prm.q_n;
-  const T* k = static_cast<const T*>(prm.k) + b * prm.k_b + g * prm.k_h;
-  const T* v = static_cast<const T*>(prm.v) + b * prm.v_b + g * prm.v_h;
-  __syncthreads();                              // (the rows before have been worked off)
-  window_rows_to_smem<T, D>(sq, q, prm.q_n, rows, tid);
-
-  float o[4][D / 64][4], m[4], l[4];
+    // (the last rows of a causal sequence see most: first)
+    const int r0 = (blocks - 1 - (int)(idx % blocks)) * M, bh = (int)(idx / blocks), b = bh / prm.heads_q, h = bh % prm.heads_q;
+    const WindowItem it(prm, b);
+    if (r0 >= it.len_q) continue;
+    if (prm.redo) {
+      const int32_t* marks = prm.redo + ((size_t)bh * ((prm.n_q + kWindowBlock - 1) / kWindowBlock) + r0 / kWindowBlock) * 16 + r0 % kWindowBlock / 16;
+      int any = 0;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    m[i] = -INFINITY;
-    l[i] = 0.f;
-#pragma unroll
-    for (int c = 0; c < D / 64; ++c)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) o[i][c][e] = 0.f;
-  }
-#pragma unroll 1
-  for (int t = 0; t < span.tiles; ++t) {
-    const int j0 = span.tile(t) * kWrKeys, keys = min(kWrKeys, it.len_k - j0);
-    __syncthreads();
-    window_rows_to_smem<T, D>(sk, k + j0 * prm.k_n, prm.k_n, keys, tid);
-    window_rows_to_smem<T, D>(sv, v + j0 * prm.v_n, prm.v_n, keys, tid);
-    __syncthreads();
-    // ---- scores of rows 4 ty .. 4 ty + 3, keys tx, tx + 16, ...
-    float s[4][4] = {};
-#pragma unroll 4
-    for (int c = 0; c < D; c += 4) {
-      float4 a[4], x[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) a[i] = *reinterpret_cast<const float4*>(sq + (4 * ty + i) * (D + 4) + c);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) x[j] = *reinterpret_cast<const float4*>(sk + (tx + 16 * j) * (D + 4) + c);
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) s[i][j] = fmaf(a[i].x, x[j].x, fmaf(a[i].y, x[j].y, fmaf(a[i].z, x[j].z, fmaf(a[i].w, x[j].w, s[i][j]))));
+      for (int i = 0; i < M / 16; ++i) any |= r0 + 16 * i < it.len_q ? marks[i] : 0;
+      if (any == 0) continue;
     }
-    const bool whole = span.whole(j0, j0 + kWrKeys);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const WindowRow row(prm, it, r0 + 4 * ty + i);
-      bool seen[4];
-      float top = m[i];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        seen[j] = whole || row.sees(j0 + tx + 16 * j);
-        s[i][j] = seen[j] ? s[i][j] * prm.scale_log2 : -INFINITY;
-        top = fmaxf(top, s[i][j]);
-      }
-#pragma unroll
-      for (int x = 1; x < 16; x <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
-      const float by = m[i] == -INFINITY ? 0.f : ptx::ex2_approx(m[i] - top), ref = top == -INFINITY ? 0.f : top;
-      m[i] = top;
-      l[i] *= by;
-#pragma unroll
-      for (int c = 0; c < D / 64; ++c)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) o[i][c][e] *= by;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const float p = ptx::ex2_approx(s[i][j] - ref);
-        if (seen[j]) l[i] += p;
-        sp[(4 * ty + i) * (kWrKeys + 4) + tx + 16 * j] = seen[j] ? p : -1.f;    // (no probability: takes no part)
-      }
-    }
-    __syncwarp();                                          // the rows of a warp's probabilities are its own
-    auto values = [&](auto masked) {
-#pragma unroll 2
-      for (int j = 0; j < kWrKeys; j += 4) {
-        float p[4][4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) *reinterpret_cast<float4*>(p[i]) = *reinterpret_cast<const float4*>(sp + (4 * ty + i) * (kWrKeys + 4) + j);
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-#pragma unroll
-          for (int c = 0; c < D / 64; ++c) {
-            const float4 x = *reinterpret_cast<const float4*>(sv + (j + e) * (D + 4) + c * 64 + tx * 4);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              if (decltype(masked)::value && p[i][e] == -1.f) continue;
-              o[i][c][0] = fmaf(p[i][e], x.x, o[i][c][0]);
-              o[i][c][1] = fmaf(p[i][e], x.y, o[i][c][1]);
-              o[i][c][2] = fmaf(p[i][e], x.z, o[i][c][2]);
-              o[i][c][3] = fmaf(p[i][e], x.w, o[i][c][3]);
-            }
-          }
-      }
+    const int rows = min(M, it.len_q - r0);
+    const WindowSpan span(prm, it, r0, r0 + rows, kWrKeys);
+    const int g = h / prm.group;
+    const T* q = static_cast<const T*>(prm.q) + b * prm.q_b + h * prm.q_h + r0 * prm.q_n;
+    const T* k = static_cast<const T*>(prm.k) + b * prm.k_b + g * prm.k_h;
+    const T* v = static_cast<const T*>(prm.v) + b * prm.v_b + g * prm.v_h;
+    auto fetch = [&](int t) {
+      const int j0 = span.tile(t) * kWrKeys, keys = it.len_k - j0;
+      float* to = smf + C::OFF_KV + (t & 1) * 2 * C::KV;
+      window_rows_to_smem<T, D, C::THREADS, kWrKeys>(to, k + j0 * prm.k_n, prm.k_n, keys, tid);
+      window_rows_to_smem<T, D, C::THREADS, kWrKeys>(to + C::KV, v + j0 * prm.v_n, prm.v_n, keys, tid);
     };
-    if (whole) values(std::false_type{});
-    else values(std::true_type{});
-  }
+    auto arrived = [&]() {
+      if (std::is_same<T, float>::value) asm volatile("cp.async.wait_all;" ::: "memory");
+      __syncthreads();
+    };
+    __syncthreads();                            // the rows before have been worked off
+    window_rows_to_smem<T, D, C::THREADS, M>(sq, q, prm.q_n, rows, tid);
+    if (span.tiles > 0) fetch(0);
+
+    f32x2 o[R][D / 32][2];
+    float m[R], l[R];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < R; ++i) {
+      m[i] = -INFINITY;
+      l[i] = 0.f;
 #pragma unroll
-    for (int x = 1; x < 16; x <<= 1) l[i] += __shfl_xor_sync(0xffffffffu, l[i], x);
-    const int row = r0 + 4 * ty + i;
-    if (row >= it.len_q) continue;
-    // a row that sees nothing: zeros, log-sum-exp -inf
-    T* out = static_cast<T*>(prm.o) + b * prm.o_b + h * prm.o_h + row * prm.o_n;
-#pragma unroll
-    for (int c = 0; c < D / 64; ++c) {
-      float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-      if (l[i] != 0.f) x = make_float4(o[i][c][0] / l[i], o[i][c][1] / l[i], o[i][c][2] / l[i], o[i][c][3] / l[i]);
-      store4(out + c * 64 + tx * 4, x);
+      for (int c = 0; c < D / 32; ++c) o[i][c][0] = o[i][c][1] = pack2(0.f, 0.f);
     }
-    if (tx == 0 && prm.lse)
-      prm.lse[((size_t)b * prm.heads_q + h) * prm.n_q + row] = l[i] == 0.f ? -INFINITY : (m[i] + log2f(l[i])) * 0.6931471805599453f;
+#pragma unroll 1
+    for (int t = 0; t < span.tiles; ++t) {
+      const int j0 = span.tile(t) * kWrKeys;
+      arrived();                                // and the tile before has been read
+      if (t + 1 < span.tiles) fetch(t + 1);
+      const float* sk = smf + C::OFF_KV + (t & 1) * 2 * C::KV;
+      const float* sv = sk + C::KV;
+      // ---- scores of rows R ty .. R ty + R - 1, keys tx, tx + 8, ...
+      f32x2 s2[R][4];
+#pragma unroll
+      for (int i = 0; i < R; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) s2[i][j] = pack2(0.f, 0.f);
+#pragma unroll 4
+      for (int c = 0; c < D; c += 4) {
+        float4 a[R], x[4];
+#pragma unroll
+        for (int i = 0; i < R; ++i) a[i] = *reinterpret_cast<const float4*>(sq + (R * ty + i) * C::PITCH + c);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x[j] = *reinterpret_cast<const float4*>(sk + (tx + 8 * j) * C::PITCH + c);
+#pragma unroll
+        for (int i = 0; i < R; ++i)
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            s2[i][j] = fma2(pack2(a[i].z, a[i].w), pack2(x[j].z, x[j].w), fma2(pack2(a[i].x, a[i].y), pack2(x[j].x, x[j].y), s2[i][j]));
+      }
+      const bool whole = span.whole(j0, j0 + kWrKeys);
+#pragma unroll
+      for (int i = 0; i < R; ++i) {
+        const WindowRow row(prm, it, r0 + R * ty + i);
+        bool seen[4];
+        float s[4], top = m[i];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          float even, odd;
+          unpack2(s2[i][j], even, odd);
+          seen[j] = whole || row.sees(j0 + tx + 8 * j);
+          s[j] = seen[j] ? (even + odd) * prm.scale_log2 : -INFINITY;
+          top = fmaxf(top, s[j]);
+        }
+#pragma unroll
+        for (int x = 1; x < 8; x <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
+        const float by = m[i] == -INFINITY ? 0.f : ex2_approx(m[i] - top), ref = top == -INFINITY ? 0.f : top;
+        m[i] = top;
+        l[i] *= by;
+#pragma unroll
+        for (int c = 0; c < D / 32; ++c) {
+          o[i][c][0] = mul2(o[i][c][0], pack2(by, by));
+          o[i][c][1] = mul2(o[i][c][1], pack2(by, by));
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float p = ex2_approx(s[j] - ref);
+          if (seen[j]) l[i] += p;
+          sp[(R * ty + i) * C::P_PITCH + tx + 8 * j] = seen[j] ? p : -1.f;      // (no probability: takes no part)
+        }
+      }
+      __syncwarp();                             // the rows of a warp's probabilities are its own
+      auto values = [&](auto masked) {
+#pragma unroll 2
+        for (int j = 0; j < kWrKeys; j += 4) {
+          float p[R][4];
+#pragma unroll
+          for (int i = 0; i < R; ++i) *reinterpret_cast<float4*>(p[i]) = *reinterpret_cast<const float4*>(sp + (R * ty + i) * C::P_PITCH + j);
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+#pragma unroll
+            for (int c = 0; c < D / 32; ++c) {
+              const float4 x = *reinterpret_cast<const float4*>(sv + (j + e) * C::PITCH + c * 32 + tx * 4);
+#pragma unroll
+              for (int i = 0; i < R; ++i) {
+                if (decltype(masked)::value && p[i][e] == -1.f) continue;
+                o[i][c][0] = fma2(pack2(p[i][e], p[i][e]), pack2(x.x, x.y), o[i][c][0]);
+                o[i][c][1] = fma2(pack2(p[i][e], p[i][e]), pack2(x.z, x.w), o[i][c][1]);
+              }
+            }
+        }
+      };
+      if (whole) values(std::false_type{});
+      else values(std::true_type{});
+    }
+    if (std::is_same<T, float>::value) asm volatile("cp.async.wait_all;" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+#pragma unroll
+      for (int x = 1; x < 8; x <<= 1) l[i] += __shfl_xor_sync(0xffffffffu, l[i], x);
+      const int row = r0 + R * ty + i;
+      if (row >= it.len_q) continue;
+      // a row that sees nothing: zeros, log-sum-exp -inf
+      T* out = static_cast<T*>(prm.o) + b * prm.o_b + h * prm.o_h + row * prm.o_n;
+#pragma unroll
+      for (int c = 0; c < D / 32; ++c) {
+        float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (l[i] != 0.f) {
+          unpack2(o[i][c][0], x.x, x.y);
+          unpack2(o[i][c][1], x.z, x.w);
+          x = make_float4(x.x / l[i], x.y / l[i], x.z / l[i], x.w / l[i]);
+        }
+        store4(out + c * 32 + tx * 4, x);
+      }
+      if (tx == 0 && prm.lse)
+        prm.lse[((size_t)b * prm.heads_q + h) * prm.n_q + row] = l[i] == 0.f ? -INFINITY : (m[i] + log2f(l[i])) * 0.6931471805599453f;
+    }
   }
-  }
+}
+
+template <typename T, int D, int M>
+static int launch_window_ref_m(const WindowParams& prm, LaunchStream st) {
+  using C = WrCfg<D, M>;
+  auto kernel = window_ref_kernel<T, D, M>;
+  CA_RETURN_IF_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM));
+  const long long n_work = (long long)ceil_div(prm.n_q, M) * prm.heads_q * prm.batch;
+  // a CTA for every tile of rows; to compute rows again, hardly ever any, as many as are on the GPU at a time
+  const long long most = prm.redo ? 296 : 0x7fffffffLL;
+  launch_chained(kernel, (unsigned)(n_work < most ? n_work : most), C::THREADS, C::SMEM, st, prm);
+  CA_LAUNCH_CHECK();
+  return CA_OK;
 }
 
 template <typename T, int D>
 static int launch_window_ref_d(const WindowParams& prm, LaunchStream st) {
-  constexpr int smem = (3 * 64 * (D + 4) + 64 * (kWrKeys + 4)) * 4;
-  auto kernel = window_ref_kernel<T, D>;
-  CA_RETURN_IF_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
-  const long long n_work = (long long)ceil_div(prm.n_q, kWrRows) * prm.heads_q * prm.batch;
-  // a CTA for every 64 rows; to compute rows again, hardly ever any, as many as are on the GPU at a time
-  const long long most = prm.redo ? 296 : 0x7fffffffLL;
-  launch_chained(kernel, (unsigned)(n_work < most ? n_work : most), kWrThreads, smem, st, prm);
-  CA_LAUNCH_CHECK();
-  return CA_OK;
+  if (!prm.redo && (long long)ceil_div(prm.n_q, 64) * prm.heads_q * prm.batch < 148) return launch_window_ref_m<T, D, 32>(prm, st);
+  return launch_window_ref_m<T, D, 64>(prm, st);
 }
 
 int launch_window_ref(const WindowParams& prm, int D, int dtype, LaunchStream st) {
@@ -189,9 +248,53 @@ int launch_window_ref(const WindowParams& prm, int D, int dtype, LaunchStream st
   return D == 64 ? launch_window_ref_d<float, 64>(prm, st) : launch_window_ref_d<float, 128>(prm, st);
 }
 
+// Blocks of rows before each batch item, counters and status: one CTA.
+__global__ void __launch_bounds__(256) window_prepare_kernel(const __grid_constant__ WindowParams prm) {
+  wait_for_previous();
+  let_next_start();
+  __shared__ int warp_sum[8];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  int bad = 0, before = 0;
+  for (int base = 0; base < prm.batch; base += 256) {
+    const int b = base + tid;
+    int v = 0;
+    if (b < prm.batch) {
+      bad |= (prm.len_q && (unsigned)prm.len_q[b] > (unsigned)prm.n_q) || (prm.len_k && (unsigned)prm.len_k[b] > (unsigned)prm.n_k);
+      v = (WindowItem(prm, b).len_q + kWindowBlock - 1) / kWindowBlock;
+    }
+    for (int d = 1; d < 32; d <<= 1) {
+      const int o = __shfl_up_sync(0xffffffffu, v, d);
+      if (lane >= d) v += o;
+    }
+    if (lane == 31) warp_sum[warp] = v;
+    __syncthreads();
+    int all = 0;
+    for (int w = 0; w < 8; ++w) {
+      if (w < warp) v += warp_sum[w];
+      all += warp_sum[w];
+    }
+    if (b < prm.batch) prm.pieces[b + 1] = before + v;
+    before += all;
+    __syncthreads();
+  }
+  bad = __syncthreads_or(bad);
+  if (tid == 0) {
+    prm.pieces[0] = 0;
+    prm.status[0] = bad ? CA_ERR_BAD_INDEX : CA_OK;
+    prm.status[kNextWord] = 0;
+    prm.status[kRedoWord] = 0;
+  }
+}
+
+int launch_window_prepare(const WindowParams& prm, LaunchStream st) {
+  launch_chained(window_prepare_kernel, 1, 256, 0, st, prm);
+  CA_LAUNCH_CHECK();
+  return CA_OK;
+}
+
 size_t window_workspace_bytes(const ca_window_t& p) {
   // status block, blocks of rows of every batch item, marks of the rows to compute again
-  return kStatusBytes + align_up(((size_t)p.batch + 1) * sizeof(int32_t), 256) + align_up((size_t)p.batch * p.heads_q * ceil_div(p.n_q, kWindowBlock) * 8 * sizeof(int32_t), 256);
+  return kStatusBytes + align_up(((size_t)p.batch + 1) * sizeof(int32_t), 256) + align_up((size_t)p.batch * p.heads_q * ceil_div(p.n_q, kWindowBlock) * 16 * sizeof(int32_t), 256);
 }
 
 int launch_window(const ca_window_t& p, const ca_rows_t* Q, const ca_rows_t* K, const ca_rows_t* V, const int32_t* len_q,
@@ -211,11 +314,11 @@ int launch_window(const ca_window_t& p, const ca_rows_t* Q, const ca_rows_t* K, 
     Carver c(ws);
     c.take<int>(kStatusBytes / sizeof(int));
     prm.pieces = c.take<int32_t>((size_t)p.batch + 1);
-    prm.redo = c.take<int32_t>((size_t)p.batch * p.heads_q * ceil_div(p.n_q, kWindowBlock) * 8);
+    prm.redo = c.take<int32_t>((size_t)p.batch * p.heads_q * ceil_div(p.n_q, kWindowBlock) * 16);
     const int rc = launch_window_tc(prm, p.head_dim, st);
     if (rc == CA_OK) return launch_window_ref(prm, p.head_dim, p.dtype, st);
     if (rc != CA_ERR_UNSUPPORTED) return rc;
-    prm.redo = nullptr;                         // strides of a broadcast: on the CUDA cores
+    prm.redo = nullptr;                         // strides of a broadcast, or too many pieces: on the CUDA cores
   }
   return launch_window_ref(prm, p.head_dim, p.dtype, st);
 }

@@ -90,44 +90,6 @@ __device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map
       : "memory");
 }
 
-// Blocks of rows before each batch item, counters and status: one CTA.
-__global__ void __launch_bounds__(256) window_prepare_kernel(const __grid_constant__ WindowParams prm) {
-  wait_for_previous();
-  let_next_start();
-  __shared__ int warp_sum[8];
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  int bad = 0, before = 0;
-  for (int base = 0; base < prm.batch; base += 256) {
-    const int b = base + tid;
-    int v = 0;
-    if (b < prm.batch) {
-      bad |= (prm.len_q && (unsigned)prm.len_q[b] > (unsigned)prm.n_q) || (prm.len_k && (unsigned)prm.len_k[b] > (unsigned)prm.n_k);
-      v = (WindowItem(prm, b).len_q + kWindowBlock - 1) / kWindowBlock;
-    }
-    for (int d = 1; d < 32; d <<= 1) {
-      const int o = __shfl_up_sync(0xffffffffu, v, d);
-      if (lane >= d) v += o;
-    }
-    if (lane == 31) warp_sum[warp] = v;
-    __syncthreads();
-    int all = 0;
-    for (int w = 0; w < 8; ++w) {
-      if (w < warp) v += warp_sum[w];
-      all += warp_sum[w];
-    }
-    if (b < prm.batch) prm.pieces[b + 1] = before + v;
-    before += all;
-    __syncthreads();
-  }
-  bad = __syncthreads_or(bad);
-  if (tid == 0) {
-    prm.pieces[0] = 0;
-    prm.status[0] = bad ? CA_ERR_BAD_INDEX : CA_OK;
-    prm.status[kNextWord] = 0;
-    prm.status[kRedoWord] = 0;
-  }
-}
-
 __device__ __forceinline__ f32x2 exp2_unit(f32x2 x) {
   float a, b;
   unpack2(x, a, b);
@@ -659,10 +621,11 @@ window_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
       }
       if (live && prm.w.lse)
         prm.w.lse[((size_t)w.b * prm.w.heads_q + w.h) * prm.w.n_q + r] = empty ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
-      // rows to be computed again: a word for each 32
+      // rows to be computed again: two words for 32 rows
       const bool again = __any_sync(0xffffffffu, live && !empty && !(fabsf(any) < INFINITY && l < INFINITY));
       if (lane == 0) {
-        prm.w.redo[((size_t)(w.b * prm.w.heads_q + w.h) * prm.blocks + w.r0 / kWtRows) * 8 + i * 4 + quarter] = again ? 1 : 0;
+        int32_t* mark = prm.w.redo + ((size_t)(w.b * prm.w.heads_q + w.h) * prm.blocks + w.r0 / kWtRows) * 16 + (i * 4 + quarter) * 2;
+        mark[0] = mark[1] = again ? 1 : 0;
         if (again) atomicExch(prm.w.status + kRedoWord, 1);
         mbar_arrive(b_work_empty(n));
       }
@@ -737,8 +700,8 @@ int launch_window_tc(const WindowParams& w, int D, LaunchStream st) {
   prm.wait_limit = kWaitLimitCycles;
   prm.wide = (reinterpret_cast<uintptr_t>(w.o) % 32 == 0) && (w.batch == 1 || w.o_b % 16 == 0) && (w.heads_q == 1 || w.o_h % 16 == 0) &&
              (w.n_q == 1 || w.o_n % 16 == 0);
-  launch_chained(window_prepare_kernel, 1, 256, 0, st, w);
-  CA_LAUNCH_CHECK();
+  const int rc = launch_window_prepare(w, st);
+  if (rc != CA_OK) return rc;
   return D == 64 ? launch_window_tc_d<64>(maps, prm, (int)n_work, st) : launch_window_tc_d<128>(maps, prm, (int)n_work, st);
 }
 
