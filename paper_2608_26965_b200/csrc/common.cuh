@@ -75,6 +75,17 @@ inline void launch_chained(void (*kernel)(Params...), dim3 grid, dim3 block, siz
   (void)cudaLaunchKernelEx(&cfg, kernel, Params(args)...);      // CA_LAUNCH_CHECK picks up an error
 }
 
+// Multiprocessors of the current device, asked for once per device (0 on error).
+inline int multiprocessors(int* device = nullptr) {
+  static std::atomic<int> known[64];
+  int dev = 0, n = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 0;
+  if (device) *device = dev;
+  n = known[dev].load(std::memory_order_relaxed);
+  if (n == 0 && cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) == cudaSuccess) known[dev].store(n, std::memory_order_relaxed);
+  return n;
+}
+
 // Per-kernel-group device times (ca_profile / ca_profile_read of the public header).  A scope
 // records a pair of CUDA events around the launches it encloses when profiling is on.
 enum ProfGroup {

@@ -729,9 +729,8 @@ size_t paged_workspace_bytes(const ca_cache_t& c) { return carve_paged(c, nullpt
 template <typename W, int D>
 static int launch_paged_d(PagedParams& prm, LaunchStream st) {
   using C = PagedCfg<W, D>;
-  int dev = 0, sms = 0;
-  CA_RETURN_IF_CUDA(cudaGetDevice(&dev));
-  CA_RETURN_IF_CUDA(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
+  const int sms = multiprocessors();
+  if (sms == 0) return CA_ERR_CUDA;
   prm.row_tiles = ceil_div(prm.group, W::ROWS);
   const int smem = C::smem(prm.group);
   auto kernel = paged_kernel<W, D>;

@@ -184,15 +184,16 @@ __global__ void __launch_bounds__(256) rotary_kernel(const __grid_constant__ Rot
   if (PAGED && blockIdx.x == 0 && blockIdx.y == 0) {
     // This block looks at every index of the call and writes the status word, so that nothing has to clear it first.
     int bad = 0;
-    const int most = prm.n / prm.page_rows + 2;
-    for (long long e = threadIdx.x; e < (long long)prm.batch * most; e += blockDim.x) {
-      const int s = (int)(e / most), part = (int)(e % most);
+    const unsigned most = (unsigned)(prm.n / prm.page_rows + 2);
+#pragma unroll 4
+    for (unsigned long long e = threadIdx.x; e < (unsigned long long)prm.batch * most; e += blockDim.x) {
+      const unsigned s = e <= 0xffffffffULL ? (unsigned)e / most : (unsigned)(e / most), part = (unsigned)(e - (unsigned long long)s * most);
       const int start = prm.lengths[s], count = prm.count ? prm.count[s] : prm.n;
       bad |= start < 0 || count < 0 || count > prm.n;
-      const long long first = max(start, 0), last = first + min(max(count, 0), prm.n) - 1;
-      const long long page = first / prm.page_rows + part;
-      if (page > last / prm.page_rows || last < first) continue;
-      if (page >= prm.pages_per_sequence) bad = 1;
+      const int rows = min(max(count, 0), prm.n);
+      const unsigned first = (unsigned)max(start, 0), page = first / (unsigned)prm.page_rows + part;
+      if (rows == 0 || page > (first + (unsigned)rows - 1u) / (unsigned)prm.page_rows) continue;
+      if (page >= (unsigned)prm.pages_per_sequence) bad = 1;
       else bad |= (unsigned)prm.page_table[(size_t)s * prm.pages_per_sequence + page] >= (unsigned)prm.pages;
     }
     bad = __syncthreads_or(bad);

@@ -70,6 +70,7 @@ struct WindowRow {
 // The tensor-core kernel wants window_prepare before it (pieces, counters and status), and window_ref behind it, with `redo` set, for
 // the rows that it marked.
 int launch_window_prepare(const WindowParams& prm, LaunchStream st);
+int launch_window_f32(const WindowParams& prm, int D, LaunchStream st);
 int launch_window_ref(const WindowParams& prm, int D, int dtype, LaunchStream st);
 int launch_window_tc(const WindowParams& prm, int D, LaunchStream st);    // CA_ERR_UNSUPPORTED: strides that it does not take
 

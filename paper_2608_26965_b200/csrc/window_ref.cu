@@ -310,12 +310,18 @@ int launch_window(const ca_window_t& p, const ca_rows_t* Q, const ca_rows_t* K, 
   prm.batch = p.batch; prm.heads_q = p.heads_q; prm.heads_kv = p.heads_kv; prm.group = p.heads_q / p.heads_kv;
   prm.n_q = p.n_q; prm.n_k = p.n_k; prm.left = p.left; prm.right = p.right; prm.sinks = p.sinks;
   prm.scale_log2 = scale * 1.4426950408889634f;
-  if (p.dtype == CA_DTYPE_BF16 && !(p.flags & CA_ATTN_FP32)) {
+  if (!(p.flags & CA_ATTN_FP32)) {
     Carver c(ws);
     c.take<int>(kStatusBytes / sizeof(int));
     prm.pieces = c.take<int32_t>((size_t)p.batch + 1);
     prm.redo = c.take<int32_t>((size_t)p.batch * p.heads_q * ceil_div(p.n_q, kWindowBlock) * 16);
-    const int rc = launch_window_tc(prm, p.head_dim, st);
+    int rc;
+    if (p.dtype == CA_DTYPE_BF16) {
+      rc = launch_window_tc(prm, p.head_dim, st);
+    } else {
+      rc = launch_window_prepare(prm, st);
+      if (rc == CA_OK) rc = launch_window_f32(prm, p.head_dim, st);
+    }
     if (rc == CA_OK) return launch_window_ref(prm, p.head_dim, p.dtype, st);
     if (rc != CA_ERR_UNSUPPORTED) return rc;
     prm.redo = nullptr;                         // strides of a broadcast, or too many pieces: on the CUDA cores

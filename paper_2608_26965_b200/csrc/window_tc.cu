@@ -634,6 +634,10 @@ window_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
   let_next_start();
   tc_fence_before();
   __syncthreads();
+  if (*abort_flag) {                       // a wait gave up: copies in flight land before the CTA's shared memory is another's
+    const long long t0 = clock64();
+    while (clock64() - t0 < 2000000) __nanosleep(1000);
+  }
   if (warp == 1) tmem_dealloc(tmem_base, 512);
 }
 
@@ -671,9 +675,8 @@ static bool rows_map(CUtensorMap* map, const void* base, int D, int n, int heads
 template <int D>
 static int launch_window_tc_d(const CUtensorMap* maps, const WtParams& prm, int n_work, LaunchStream st) {
   auto kernel = window_tc_kernel<D>;
-  int dev = 0, sms = 0;
-  CA_RETURN_IF_CUDA(cudaGetDevice(&dev));
-  CA_RETURN_IF_CUDA(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
+  const int sms = multiprocessors();
+  if (sms == 0) return CA_ERR_CUDA;
   CA_RETURN_IF_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, WtCfg<D>::SMEM));
   launch_chained(kernel, n_work < sms ? n_work : sms, kWtThreads, WtCfg<D>::SMEM, st, maps[0], maps[1], maps[2], prm);
   CA_LAUNCH_CHECK();
@@ -697,7 +700,8 @@ int launch_window_tc(const WindowParams& w, int D, LaunchStream st) {
   // causal sequence even out the end of the call.
   const double reach = (w.left < 0 ? w.n_k : fmin((double)w.n_k, (double)w.left + (w.right < 0 ? w.n_k : w.right) + 2.0 * kWtRows));
   prm.rows_first = (double)w.batch * w.heads_kv * reach * D * 4 < 80e6;
-  prm.wait_limit = kWaitLimitCycles;
+  // A wait for the next piece can be as long as a piece: 20 us for every step of one, which takes 2, on top of the usual limit.
+  prm.wait_limit = kWaitLimitCycles + (long long)(fmin(reach + w.sinks, (double)w.n_k) / kWtKeys + 4) * 40000;
   prm.wide = (reinterpret_cast<uintptr_t>(w.o) % 32 == 0) && (w.batch == 1 || w.o_b % 16 == 0) && (w.heads_q == 1 || w.o_h % 16 == 0) &&
              (w.n_q == 1 || w.o_n % 16 == 0);
   const int rc = launch_window_prepare(w, st);
