@@ -370,9 +370,10 @@ int paged_attention_fwd(const ca_cache_t* c, const ca_rows_t* Q, const void* K_p
  * (right = 0: causal; first tokens that stand behind p + right are not seen).  O = softmax-weighted mean of
  * the visible values, lse [batch, heads_q, n_q] fp32 or NULL; a row that sees nothing: zeros and -inf.  Rows from
  * len_q[b] on are left as they were, in O and lse, and rows of K and V from len_k[b] on are not used.
- * bf16 storage runs on tcgen05 tensor cores with fp32 accumulation and bf16 probabilities (CA_ATTN_FP32 in
- * flags, or fp32 storage: the FP32 CUDA-core kernel).  A length out of range is cut to it and
- * CA_ERR_BAD_INDEX recorded.
+ * bf16 storage runs on tcgen05 tensor cores with fp32 accumulation and bf16 probabilities, fp32 storage on
+ * products of tf32 halves with the accuracy of fp32; CA_ATTN_FP32 in flags selects the FP32 CUDA-core kernel,
+ * and it computes again what a tensor core gives as not finite, so that masked values may be anything.  A
+ * length out of range is cut to it and CA_ERR_BAD_INDEX recorded.
  */
 typedef struct {
   int32_t batch, heads_q, heads_kv;

@@ -14,6 +14,7 @@ struct WindowParams {
   int32_t* pieces;                  // [batch + 1] blocks of kWindowBlock rows of the batch items before
   int32_t* redo;                    // [batch * heads_q][blocks of kWindowBlock rows][16]: 16 rows each, to be computed again (null: all)
   int batch, heads_q, heads_kv, group, n_q, n_k, left, right, sinks;
+  int one_each;                     // no lengths, and a CTA of the tensor-core kernel for every block of rows: nothing is prepared for it
   float scale_log2;
 };
 
@@ -67,11 +68,11 @@ struct WindowRow {
   __device__ __forceinline__ bool sees(int j) const { return j < end && (j >= from || j < sinks); }
 };
 
-// The tensor-core kernel wants window_prepare before it (pieces, counters and status), and window_ref behind it, with `redo` set, for
-// the rows that it marked.
+// The tensor-core kernels want window_prepare before them (pieces, counters and status; the bf16 kernel sees to it), and window_ref
+// behind them, with `redo` set, for the rows that they marked.
 int launch_window_prepare(const WindowParams& prm, LaunchStream st);
 int launch_window_f32(const WindowParams& prm, int D, LaunchStream st);
 int launch_window_ref(const WindowParams& prm, int D, int dtype, LaunchStream st);
-int launch_window_tc(const WindowParams& prm, int D, LaunchStream st);    // CA_ERR_UNSUPPORTED: strides that it does not take
+int launch_window_tc(WindowParams& prm, int D, LaunchStream st);    // CA_ERR_UNSUPPORTED: strides that it does not take
 
 }  // namespace ca

@@ -1,13 +1,19 @@
 // Attention over a sliding window for fp32 storage, on m16n8k8 products of tf32 operands.
 //
 // tf32 has 11 significant bits, so each operand is split in two, x = hi + lo with hi = x rounded to tf32 and lo = the rest rounded
-// to tf32, and a product is lo hi + hi lo + hi hi: what is left out is 2^-22 of it, about as much as fp32 sums lose.  That is three
-// products for one, at four times the rate of the multiply-adds of the CUDA cores, and the operands come from shared memory a
-// word per lane and product instead of eight vectors for 32 multiply-adds, which is what bounds the CUDA-core kernel
-// (window_ref.cu: 12 heads of 1,370 rows, d = 64, 148 rows to either side 67 us; here FIGURE).
+// to tf32, and a product is lo hi + hi lo + hi hi: what is left out is 2^-22 of it.  The tensor core cuts its sums instead of rounding
+// them, which over long chains loses more than that (2.7e-6 of the result with one accumulator for all); so chains of upper parts are two
+// products long and are added up in fp32, and the small products have chains of their own: 3.2e-7 off where a plain fp32 form is
+// 6e-7 (12 heads of 1,370 rows, d = 64, 148 rows to either side).
 //
-// A warp has 16 query rows, in registers as hi and lo; keys and values come 32 at a time by asynchronous copies, shared by the
-// CTA's warps, while the 32 before are worked on.
+// Three products for one, at four times the rate of the CUDA cores' multiply-adds, and the operands come from shared memory a
+// word per lane and product: the 1,370 rows take 47 us (window_ref.cu, which waits for vectors of shared memory, 73), 2 x 8 heads of 4,000
+// rows, causal, d = 64, 500 rows before 233 us (331).  What bounds it is the chain of a warp's step (copy to registers, split,
+// product, softmax, product): tensor pipe 43 % busy, an instruction every third cycle, with the eight warps that 255 registers allow (168
+// registers and twelve warps: 55 us, 128 and sixteen: 76, for the registers that then go through memory).
+//
+// A warp has 16 query rows in registers, a CTA four warps; keys and values come 32 at a time by asynchronous copies, shared by the
+// warps, while the 32 before are worked on.
 //     S = Q K^T      a thread holds rows lane/4 and lane/4 + 8, keys 2 (lane % 4) and the next of every 8
 //     O += P V       P as it is held: its keys 2 t and 2 t + 1 stand at columns t and t + 4 of the product, and V's rows likewise
 // Masked probabilities are 0, and 0 x infinity is not: rows whose result is not finite are marked and computed again by the
@@ -21,7 +27,7 @@ namespace ca {
 
 using namespace ptx;
 
-constexpr int kWfKeys = 32;
+constexpr int kWfKeys = 32, kWfRows = 64, kWfThreads = 128;
 
 template <int D>
 struct WfCfg {
@@ -42,25 +48,24 @@ __device__ __forceinline__ Split split(float x) {
   return s;
 }
 __device__ __forceinline__ void mma1688(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-  asm volatile("mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+  asm("mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-template <int D, int WARPS>
-__global__ void __launch_bounds__(WARPS * 32) window_f32_kernel(const __grid_constant__ WindowParams prm) {
+template <int D>
+__global__ void __launch_bounds__(kWfThreads) window_f32_kernel(const __grid_constant__ WindowParams prm) {
   wait_for_previous();
   let_next_start();
   using C = WfCfg<D>;
-  constexpr int M = 16 * WARPS, THREADS = 32 * WARPS;
   extern __shared__ __align__(16) float smf[];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t4 = lane & 3;
-  const int blocks = (prm.n_q + M - 1) / M;
+  const int blocks = (prm.n_q + kWfRows - 1) / kWfRows;
   // (the last rows of a causal sequence see most: first)
-  const int r0 = (blocks - 1 - (int)(blockIdx.x % blocks)) * M, bh = blockIdx.x / blocks, b = bh / prm.heads_q, h = bh % prm.heads_q;
+  const int r0 = (blocks - 1 - (int)(blockIdx.x % blocks)) * kWfRows, bh = blockIdx.x / blocks, b = bh / prm.heads_q, h = bh % prm.heads_q;
   const WindowItem it(prm, b);
   if (r0 >= it.len_q) return;
-  const WindowSpan span(prm, it, r0, min(r0 + M, it.len_q), kWfKeys);
+  const WindowSpan span(prm, it, r0, min(r0 + kWfRows, it.len_q), kWfKeys);
   const int kv = h / prm.group;
   const float* k = static_cast<const float*>(prm.k) + b * prm.k_b + kv * prm.k_h;
   const float* v = static_cast<const float*>(prm.v) + b * prm.v_b + kv * prm.v_h;
@@ -68,7 +73,7 @@ __global__ void __launch_bounds__(WARPS * 32) window_f32_kernel(const __grid_con
     const int j0 = span.tile(t) * kWfKeys;
     const uint32_t to = smem_u32(smf + (t & 1) * 2 * C::TILE);
 #pragma unroll
-    for (int i = tid; i < kWfKeys * D / 4; i += THREADS) {
+    for (int i = tid; i < kWfKeys * D / 4; i += kWfThreads) {
       const int r = i / (D / 4), c = i % (D / 4) * 4;
       const bool there = j0 + r < it.len_k;
       const uint32_t at = to + (r * C::PITCH + c) * 4;
@@ -223,22 +228,19 @@ __global__ void __launch_bounds__(WARPS * 32) window_f32_kernel(const __grid_con
   }
 }
 
-template <int D, int WARPS>
+template <int D>
 static int launch_window_f32_d(const WindowParams& prm, LaunchStream st) {
-  auto kernel = window_f32_kernel<D, WARPS>;
+  auto kernel = window_f32_kernel<D>;
   CA_RETURN_IF_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, WfCfg<D>::SMEM));
-  const long long n_work = (long long)ceil_div(prm.n_q, 16 * WARPS) * prm.heads_q * prm.batch;
+  const long long n_work = (long long)ceil_div(prm.n_q, kWfRows) * prm.heads_q * prm.batch;
   if (n_work > 0x7fffffffLL) return CA_ERR_UNSUPPORTED;
-  launch_chained(kernel, (unsigned)n_work, 32 * WARPS, WfCfg<D>::SMEM, st, prm);
+  launch_chained(kernel, (unsigned)n_work, kWfThreads, WfCfg<D>::SMEM, st, prm);
   CA_LAUNCH_CHECK();
   return CA_OK;
 }
 
 int launch_window_f32(const WindowParams& prm, int D, LaunchStream st) {
-  // four warps to a CTA, two where that would be fewer than four CTAs to an SM
-  const bool few = (long long)ceil_div(prm.n_q, 64) * prm.heads_q * prm.batch < 4 * 148;
-  if (D == 64) return few ? launch_window_f32_d<64, 2>(prm, st) : launch_window_f32_d<64, 4>(prm, st);
-  return few ? launch_window_f32_d<128, 2>(prm, st) : launch_window_f32_d<128, 4>(prm, st);
+  return D == 64 ? launch_window_f32_d<64>(prm, st) : launch_window_f32_d<128>(prm, st);
 }
 
 }  // namespace ca

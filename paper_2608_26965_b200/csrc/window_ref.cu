@@ -1,15 +1,13 @@
-// Attention over a sliding window on the CUDA cores, in fp32: fp32 storage, and the rows that the tensor-core kernel
-// leaves to it.
+// Attention over a sliding window on the CUDA cores, in fp32: the rows that the tensor-core kernels leave to it, strides that they do not
+// take, and CA_ATTN_FP32.
 //     S = Q K^T, P = exp2(S c - m) over the visible keys, O = P V / sum P,    m the running maximum of a row.
 // A CTA takes M query rows and goes over the keys that they see, 32 at a time, which arrive while the 32 before are worked on (fp32
 // storage).  A thread has R x 4 scores and R x D/8 columns of the result in registers.  What bounds it is reading shared memory, not the
-// multiply-adds (two to an instruction): a vector of 16 bytes per lane takes the 3.6 cycles of four whether lanes read the same
+// multiply-adds (two to an instruction): a vector of 16 bytes per lane takes 3.6 cycles whether lanes read the same
 // one or not, so 8 vectors for 32 instructions (R = 4) keep the reads of four warps at it for 115 cycles and the multiply-adds
 // for 64.  2 x 8 heads of 4,000 rows, causal, d = 128: 2.08 ms, 31 TFLOP/s of visible pairs (R = 2 2.93 ms; R = 8 3.19, for want of
-// registers and warps).  12 heads of 1,370 rows, d = 64, 148 rows to either side: 73 us.  M = 64 with R = 4; M = 32 with R = 2 where
-// tiles of 64 rows would be fewer than one to an SM (100 rows, one head: 10.4 us instead of 15.4).
-// (Products of tf32 halves on the tensor cores, three for one, took 56 us for the 1,370 rows, but their sums are cut instead of rounded:
-// 2.7e-6 off where this kernel and a plain one are 6.4e-7.)
+// registers and warps).  M = 64 with R = 4; M = 32 with R = 2 where tiles of 64 rows would be fewer than one to an SM (100 rows, one
+// head: 10.4 us instead of 15.4).
 // Only tiles at a border of the window are masked: what a row does not see takes no part, whatever stands there
 // (0 x infinity would).
 #include <math.h>
@@ -64,7 +62,7 @@ __global__ void __launch_bounds__(WrCfg<D, M>::THREADS) window_ref_kernel(const 
   float* sp = smf + C::OFF_P;
   const int tid = threadIdx.x, ty = tid >> 3, tx = tid & 7;
   if (prm.redo) {
-    if (prm.status[kRedoWord] == 0) return;
+    if (!prm.one_each && prm.status[kRedoWord] == 0) return;
   } else if (blockIdx.x == 0) {
     // the only one that writes the status word
     int bad = 0;

@@ -39,8 +39,6 @@ constexpr int kWtThreads = 384;
 constexpr int kWtRows = kWindowBlock;      // query rows of a piece of work
 constexpr int kWtKeys = 128;
 
-
-
 constexpr int kWtEvery = 16;               // of every 16 columns, two take their exponentials from the FMA units
 constexpr float kE1 = 0.693147004f, kE2 = 0.240222424f, kE3 = 0.0555073358f, kE4 = 0.00967151299f, kE5 = 0.00132647273f;
 constexpr float kWtSumLimit = 4294967296.f;   // 2^32: a sum of 32 probabilities above it raises the reference
@@ -56,7 +54,7 @@ struct WtCfg {
   static constexpr int OFF_Q = 0, OFF_K = 2 * TILE_BYTES, OFF_V = OFF_K + NK * TILE_BYTES;
   static constexpr int OFF_WORK = OFF_V + NV * TILE_BYTES;    // [kWtRing] Work
   static constexpr int OFF_BAR = OFF_WORK + kWtRing * 64;
-  static constexpr int NUM_BARS = 16 + 2 * kWtRing + 2 * NK + 3 * NV;
+  static constexpr int NUM_BARS = 17 + 2 * kWtRing + 2 * NK + 3 * NV;
   static constexpr int OFF_MISC = OFF_BAR + 8 * NUM_BARS;     // tensor memory base, abort flag
   static constexpr int SMEM = 1024 + OFF_MISC + 16;
   static_assert(SMEM <= 227 * 1024, "shared memory");
@@ -140,7 +138,8 @@ window_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
   auto b_o_empty = [&](int i) { return bar0 + 112 + 8 * i; };
   auto b_work_full = [&](int n) { return bar0 + 128 + 8 * (n % kWtRing); };
   auto b_work_empty = [&](int n) { return bar0 + 128 + 8 * (kWtRing + n % kWtRing); };
-  const uint32_t bar1 = bar0 + 128 + 16 * kWtRing;
+  const uint32_t b_claim = bar0 + 128 + 16 * kWtRing;
+  const uint32_t bar1 = b_claim + 8;
   auto b_k_full = [&](int s) { return bar1 + 8 * s; };
   auto b_k_empty = [&](int s) { return bar1 + 8 * (C::NK + s); };
   auto b_v_full = [&](int s) { return bar1 + 8 * (2 * C::NK + s); };
@@ -165,6 +164,7 @@ window_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
     for (int i = 0; i < kWtRing; ++i) { mbar_init(b_work_full(i), 1); mbar_init(b_work_empty(i), 11); }
     for (int s = 0; s < C::NK; ++s) { mbar_init(b_k_full(s), 1); mbar_init(b_k_empty(s), 1); }
     for (int s = 0; s < C::NV; ++s) { mbar_init(b_v_full(s), 1); mbar_init(b_v_ready(s), 1); mbar_init(b_v_empty(s), 1); }
+    mbar_init(b_claim, 1);
     *abort_flag = 0;
     fence_mbar_init();
   }
@@ -191,9 +191,18 @@ window_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
   if (warp == 3) {
     // ---------------------------------------------------------- work
     if (lane == 0) {
-      const int all_blocks = prm.w.pieces[prm.w.batch], n_work = all_blocks * prm.w.heads_q;
+      const int all_blocks = prm.w.one_each ? prm.blocks * prm.w.batch : prm.w.pieces[prm.w.batch], n_work = all_blocks * prm.w.heads_q;
+      if (prm.w.one_each && blockIdx.x == 0) prm.w.status[0] = CA_OK;      // (a wait that gives up writes it a second later)
       int n = 0;
       for (int idx = blockIdx.x;; ++n) {
+        // A piece is claimed when the one before is nearly loaded, not earlier: what a CTA has claimed another that is done cannot take
+        // (with four claimed ahead SMs were at work for 77 % of a call of four pieces each).
+        if (n > 0 && prm.w.one_each) {
+          idx = n_work;
+        } else if (n > 0) {
+          if (!relaxed(b_claim, n - 1)) break;
+          idx = (int)gridDim.x + atomicAdd(prm.w.status + kNextWord, 1);
+        }
         Work w;
         w.b = -1;
         if (idx < n_work) {
@@ -204,15 +213,19 @@ window_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
             w.h = idx % prm.w.heads_q;
             block = all_blocks - 1 - idx / prm.w.heads_q;
           }
-          idx = (int)gridDim.x + atomicAdd(prm.w.status + kNextWord, 1);
-          int lo = 0, hi = prm.w.batch - 1;            // the batch item of the block
-          while (lo < hi) {
-            const int mid = (lo + hi + 1) >> 1;
-            if (prm.w.pieces[mid] <= block) lo = mid;
-            else hi = mid - 1;
+          if (prm.w.one_each) {
+            w.b = block / prm.blocks;
+            w.r0 = block % prm.blocks * kWtRows;
+          } else {
+            int lo = 0, hi = prm.w.batch - 1;            // the batch item of the block
+            while (lo < hi) {
+              const int mid = (lo + hi + 1) >> 1;
+              if (prm.w.pieces[mid] <= block) lo = mid;
+              else hi = mid - 1;
+            }
+            w.b = lo;
+            w.r0 = (block - prm.w.pieces[lo]) * kWtRows;
           }
-          w.b = lo;
-          w.r0 = (block - prm.w.pieces[lo]) * kWtRows;
           const WindowItem it(prm.w, w.b);
           w.len_q = it.len_q;
           w.len_k = it.len_k;
@@ -257,8 +270,10 @@ window_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
         if (w.b < 0) break;
         const int g = w.h / prm.w.group;
         bool q_there[2] = {false, false};
+        if (w.tiles == 0) mbar_arrive(b_claim);
         for (int u = 0; u < w.tiles && ok; ++u) {
           const int t = w.tile(u);
+          if (u == max(0, w.tiles - 4)) mbar_arrive(b_claim);
           // queries of the tiles that begin here: the first before the keys, which wait for less than the second
           auto queries = [&](int i) {
             if (q_there[i] || !w.active(i, t, sinks)) return;
@@ -329,7 +344,7 @@ window_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
       const uint64_t q_desc0 = smem_desc_sw128(s_q, 16, 1024);
       const uint64_t k_desc0 = smem_desc_sw128(s_k, 16, 1024);
       const uint64_t v_desc0 = smem_desc_sw128(s_v, C::PANEL_BYTES, 1024);
-      int n_s[2] = {0, 0}, n_pv[2] = {0, 0}, n_q[2] = {0, 0}, n_o[2] = {0, 0};   // steps, steps, query tiles, results so far
+      int n_pv[2] = {0, 0}, n_q[2] = {0, 0}, n_o[2] = {0, 0};   // steps, query tiles, results so far
       int k_slot = 0, v_slot = 0;
       uint32_t k_ph = 0, v_ph = 0;
       bool on[2] = {false, false};             // the step before: query tiles that take part, the first, the last of their steps
@@ -406,7 +421,6 @@ window_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
             }
             mma_commit(b_s_full(i));
             if (last[i]) mma_commit(b_q_empty(i));
-            ++n_s[i];
           } else if (on[i]) {
             mma_commit(b_pv_done(i));
             if (was_last[i]) mma_commit(b_o_full(i));
@@ -626,7 +640,7 @@ window_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
       if (lane == 0) {
         int32_t* mark = prm.w.redo + ((size_t)(w.b * prm.w.heads_q + w.h) * prm.blocks + w.r0 / kWtRows) * 16 + (i * 4 + quarter) * 2;
         mark[0] = mark[1] = again ? 1 : 0;
-        if (again) atomicExch(prm.w.status + kRedoWord, 1);
+        if (again && !prm.w.one_each) atomicExch(prm.w.status + kRedoWord, 1);
         mbar_arrive(b_work_empty(n));
       }
     }
@@ -684,7 +698,7 @@ static int launch_window_tc_d(const CUtensorMap* maps, const WtParams& prm, int 
 }
 
 // CA_ERR_UNSUPPORTED: strides that a tensor map does not describe
-int launch_window_tc(const WindowParams& w, int D, LaunchStream st) {
+int launch_window_tc(WindowParams& w, int D, LaunchStream st) {
   CUtensorMap maps[3];
   if (!rows_map(&maps[0], w.q, D, w.n_q, w.heads_q, w.batch, w.q_n, w.q_h, w.q_b) ||
       !rows_map(&maps[1], w.k, D, w.n_k, w.heads_kv, w.batch, w.k_n, w.k_h, w.k_b) ||
@@ -704,8 +718,15 @@ int launch_window_tc(const WindowParams& w, int D, LaunchStream st) {
   prm.wait_limit = kWaitLimitCycles + (long long)(fmin(reach + w.sinks, (double)w.n_k) / kWtKeys + 4) * 40000;
   prm.wide = (reinterpret_cast<uintptr_t>(w.o) % 32 == 0) && (w.batch == 1 || w.o_b % 16 == 0) && (w.heads_q == 1 || w.o_h % 16 == 0) &&
              (w.n_q == 1 || w.o_n % 16 == 0);
-  const int rc = launch_window_prepare(w, st);
-  if (rc != CA_OK) return rc;
+  const int sms = multiprocessors();
+  if (sms == 0) return CA_ERR_CUDA;
+  // A CTA for every piece, and no lengths: no counter, no list of pieces, and the marks are few enough to be looked at one by one; a
+  // launch less.
+  prm.w.one_each = w.one_each = !w.len_q && !w.len_k && n_work <= sms;
+  if (!w.one_each) {
+    const int rc = launch_window_prepare(w, st);
+    if (rc != CA_OK) return rc;
+  }
   return D == 64 ? launch_window_tc_d<64>(maps, prm, (int)n_work, st) : launch_window_tc_d<128>(maps, prm, (int)n_work, st);
 }
 

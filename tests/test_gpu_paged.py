@@ -59,7 +59,7 @@ LENGTHS = [0, 1, 2, 15, 16, 17, 31, 33, 63, 64, 65, 100, 129, 1000]
 
 
 @pytest.mark.parametrize("dtype,d", [("bf16", 64), ("bf16", 128), ("fp32", 64), ("fp32", 128)])
-@pytest.mark.parametrize("hq,kv", [(1, 1), (2, 1), (6, 2), (12, 3), (10, 2), (24, 3), (16, 1), (34, 2), (40, 1)])
+@pytest.mark.parametrize("hq,kv", [(1, 1), (2, 1), (6, 2), (12, 3), (10, 2), (24, 3), (16, 1), (12, 1), (34, 2), (40, 1)])
 @pytest.mark.parametrize("page_rows,left,sinks", [(16, -1, 0), (100, 40, 3), (17, 0, 0), (64, 200, 70)])
 def test_lengths_heads_windows(dtype, d, hq, kv, page_rows, left, sinks):
     cache, q = make(hq + page_rows, LENGTHS, hq, kv, d, dtype, page_rows, left, sinks)
@@ -235,6 +235,29 @@ def test_two_graphs_share_a_workspace_and_other_streams():
         own.paged_attention_fwd(q2, stream=streams[1])
     torch.cuda.synchronize()
     assert torch.equal(one.O, want[0]) and torch.equal(own.O, want[1])
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 64), ("bf16", 128), ("fp32", 64), ("fp32", 128)])
+def test_one_long_head_over_all_parts(dtype, d):
+    """As many parts as the GPU takes at a time for one head: more than a joining thread has loads in flight, by groups."""
+    for hq, lengths in ((1, [70001]), (3, [65536]), (16, [40000, 0, 3])):
+        cache, q = make(d + hq, lengths, hq, 1, d, dtype, 64)
+        O, lse = cache.paged_attention_fwd(q)
+        assert cache.last_status() == 0
+        check(cache, q, lengths, O, lse)
+
+
+def test_sequences_that_share_pages():
+    """A fork: two sequences read the same pages and differ in their last one."""
+    cache, q = make(8, [100, 100], 4, 2, 64, "bf16", 16, garbage=False)
+    cache.page_table[1, :6] = cache.page_table[0, :6]
+    q[1] = q[0]
+    O, lse = cache.paged_attention_fwd(q)
+    check(cache, q, [100, 100], O, lse)
+    assert not torch.equal(O[0], O[1])
+    cache.page_table[1] = cache.page_table[0]
+    O, lse = cache.paged_attention_fwd(q)
+    assert torch.equal(O[0], O[1]) and torch.equal(lse[0], lse[1])
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])

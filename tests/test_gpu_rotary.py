@@ -93,6 +93,32 @@ def test_in_place_gives_the_same(dtype, adjacent, pairs):
     assert torch.equal(q, a) and torch.equal(k, b)
 
 
+def test_broadcast_rows_and_many_batch_items():
+    """Inputs with strides of zero; more batch items than a block of threads has rows; one key head for all."""
+    g = generator(21)
+    rot = binding.Rotary(64, [8, 8], adjacent=False)
+    for dtype in DT.values():
+        q = torch.randn((1, 3, 5, 64), generator=g, device=DEV).to(dtype).expand(700, 3, 5, 64)
+        k = torch.randn((700, 1, 1, 64), generator=g, device=DEV).to(dtype).expand(700, 1, 5, 64)
+        pos = positions(g, 700, 5, 2, 1000)
+        for x, y in zip((q, k), binding.rotary_axes(rot, q, k, pos)):
+            want = ref.rotate(x.double(), pos, rot.frequencies, [8, 8], False)
+            ref.check(y, want, ref.rotate_bound(x.double(), [8, 8], False, dtype, want), "rotary")
+
+
+def test_other_stream():
+    g = generator(22)
+    rot = binding.Rotary(128, [16, 24, 24])
+    q = torch.randn((2, 8, 3000, 128), generator=g, device=DEV)
+    pos = positions(g, 2, 3000, 3, 100)
+    want = binding.rotary_axes(rot, q, None, pos)[0]
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    outs = [binding.rotary_axes(rot, q, None, pos, stream=side)[0] for _ in range(4)]
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, want) for x in outs)
+
+
 def test_inverse_is_the_gradient():
     """Against the gradient of the 64-bit form, and against differences (the map is linear, so they are exact but for rounding)."""
     g = generator(9)

@@ -10,7 +10,7 @@ from paper_2608_26965_b200 import binding
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
 DT = {"fp32": torch.float32, "bf16": torch.bfloat16}
-KERNELS = [("bf16", 0), ("bf16", binding.CA_ATTN_FP32), ("fp32", 0)]
+KERNELS = [("bf16", 0), ("bf16", binding.CA_ATTN_FP32), ("fp32", 0), ("fp32", binding.CA_ATTN_FP32)]
 
 
 def generator(seed):
@@ -235,6 +235,51 @@ def test_strides_beyond_32_bits(dtype, flags):
         x.copy_(rows(g, (2, 1, n, d), dtype))
     O, lse = run(p, q, k, v, out=out)
     check(p, q, k, v, O, lse)
+
+
+@pytest.mark.parametrize("dtype,flags", KERNELS)
+def test_broadcast_keys_and_values(dtype, flags):
+    """Keys and values that are the same for the whole batch (a stride of zero), one row of keys for all queries, one query."""
+    g = generator(31)
+    d = 64
+    for n_q, n_k, left, right in ((300, 300, 40, 10), (1, 300, -1, -1), (300, 1, -1, -1)):
+        p = binding.make_window_problem(3, 4, 2, n_q, n_k, d, dtype, left, right, 2, flags=flags)
+        q = rows(g, (3, 4, n_q, d), dtype)
+        k, v = (rows(g, (1, 2, n_k, d), dtype).expand(3, 2, n_k, d) for _ in range(2))
+        check(p, q, k, v, *run(p, q, k, v))
+        q1 = rows(g, (3, 1, n_q, d), dtype).expand(3, 4, n_q, d)
+        check(p, q1, k, v, *run(p, q1, k, v))
+
+
+def test_rows_at_any_16_bytes():
+    """Outputs and inputs that start at a multiple of 16 bytes that is none of 32."""
+    g = generator(32)
+    n, d = 300, 128
+    for dtype, flags in KERNELS:
+        p = binding.make_window_problem(1, 3, 1, n, n, d, dtype, 70, 3, 1, flags=flags)
+        step = 16 // torch.empty((), dtype=DT[dtype]).element_size()
+        room = lambda h: (torch.randn((1, h, n, d + step), generator=g, device=DEV)).to(DT[dtype])[..., step:]
+        q, k, v, out = room(3), room(1), room(1), room(3)
+        assert out.data_ptr() % 32 == 16
+        check(p, q, k, v, *run(p, q, k, v, out=out))
+
+
+def test_many_short_sequences():
+    """More pieces of work than SMs, most of a batch's rows missing, pieces of one key tile."""
+    g = generator(33)
+    B, n, d = 70, 520, 64
+    len_q = [(37 * i) % 521 for i in range(B)]
+    len_k = [(91 * i + 13) % 521 for i in range(B)]
+    for dtype, flags in KERNELS:
+        p = binding.make_window_problem(B, 4, 4, n, n, d, dtype, 100, 0, 3, flags=flags)
+        q, k, v = (rows(g, (B, 4, n, d), dtype, "rows_first") for _ in range(3))
+        plan = binding.WindowPlan(p, DEV)
+        plan.O.fill_(3.0)
+        O, lse = plan.window_attention_fwd(q, k, v, *(torch.tensor(x, dtype=torch.int32, device=DEV) for x in (len_q, len_k)))
+        assert plan.last_status() == 0
+        check(p, q, k, v, O, lse, len_q, len_k, heads=[0, 3])
+        for b in range(B):
+            assert (O[b, :, len_q[b]:] == 3.0).all()
 
 
 def test_same_results_as_one_token_at_a_time():
