@@ -514,6 +514,9 @@ def _call(fn, what: str, device: torch.device, stream: Optional[torch.cuda.Strea
         _check(rc, what)
 
 
+_SAME = contextlib.nullcontext()
+
+
 class Rotary:
     """Rotary positions: pairs[a] pairs of channels turn with axis a of a position, by `frequencies` (radians
     per step, one for every pair), or theta ** (-i / pairs[a]) for pair i of an axis.  adjacent: pair c is
@@ -563,16 +566,18 @@ def rotary_axes(rotary: Rotary, q, k, positions, inverse: bool = False, out_q=No
         b = _rows(k, "k", shape_k, dtype, device)
     elif out_k is not None:
         raise ClusterAttnError("out_k without k")
-    if out_q is None or (k is not None and out_k is None):
-        # new memory is in order with what the call's stream does
-        with contextlib.nullcontext() if stream is None else torch.cuda.stream(stream):
-            if out_q is None:
-                out_q = q.new_empty(shape)
-            if k is not None and out_k is None:
-                out_k = q.new_empty(shape_k)
-    c = _rows(out_q, "out_q", shape, dtype, device)
-    if k is not None:
+    c = _rows(out_q, "out_q", shape, dtype, device) if out_q is not None else None
+    if k is not None and out_k is not None:
         d = _rows(out_k, "out_k", shape_k, dtype, device)
+    if c is None or (k is not None and d is None):
+        # new dense memory, in order with what the call's stream does
+        with _SAME if stream is None else torch.cuda.stream(stream):
+            if c is None:
+                out_q = q.new_empty(shape)
+                c = CaRows(out_q.data_ptr(), H * n * D, n * D, D)
+            if k is not None and d is None:
+                out_k = q.new_empty(shape_k)
+                d = CaRows(out_k.data_ptr(), Hk * n * D, n * D, D)
     _call(load_library().rotary_axes, "rotary_axes", device, stream, rotary._struct, B, H, Hk, n, D, _OF_TORCH[dtype],
           1 if inverse else 0, a, b, pos, pos_b, c, d)
     return out_q, out_k

@@ -33,6 +33,8 @@ constexpr int kPagedThreads = kPagedWarps * 32;
 // What the start and the end of a (sequence, key head, row tile) cost, in units of rows: without it the parts that hold many short
 // sequences take longest (64 sequences of 1 to 8,192 rows, 8 key heads of 4 query heads, d = 128: 0 90 us, 1 61, 2 51.5, 4 53, 8 57).
 constexpr int kPairUnits = 3;
+// Caches of at most so many rows a sequence are not split: a CTA for every (sequence, key head, row tile), one launch instead of three.
+constexpr int kDirectRows = 256;
 constexpr int kPagedMaxCtas = 640;           // most CTAs of a launch: the workspace holds two partial results of each
 
 __host__ __device__ inline int ceil_div_device(int a, int b) { return (a + b - 1) / b; }
@@ -49,6 +51,7 @@ struct PagedParams {
   long long* units;              // [batch + 1] units of a (key head, row tile) of the sequences before
   float* partial;                // [2 * CTAs] O [rows][D] (not divided), {m (log2 units), l} [rows]; rows (D + 4) floats apart
   int batch, heads_q, heads_kv, group, row_tiles, page_rows, pages, pages_per_sequence, appended, left, sinks;
+  int direct;                    // a CTA for every (sequence, key head, row tile): nothing is planned or joined
   float scale_log2;
 };
 
@@ -478,11 +481,18 @@ __global__ void __launch_bounds__(kPagedThreads) paged_kernel(const __grid_const
   wait_for_previous();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int per = prm.heads_kv * prm.row_tiles;              // (key head, row tile) pairs of a sequence
-  const long long total = prm.units[prm.batch] * per;
-  const long long parts = min((long long)gridDim.x, total);
-  if (blockIdx.x >= parts) { let_next_start(); return; }
   Place at;
-  {
+  if (prm.direct) {
+    at.b = blockIdx.x / per;
+    at.h = blockIdx.x % per / prm.row_tiles;
+    at.rt = blockIdx.x % prm.row_tiles;
+    at.pos = at.end = 0;                                     // (none behind it)
+    at.tile = 0;
+    at.last = Span(prm, at.b, C::U).tiles;
+  } else {
+    const long long total = prm.units[prm.batch] * per;
+    const long long parts = min((long long)gridDim.x, total);
+    if (blockIdx.x >= parts) { let_next_start(); return; }
     const long long begin = total * blockIdx.x / parts;
     at.end = total * (blockIdx.x + 1) / parts;
     int lo = 0, hi = prm.batch - 1;                          // last sequence whose units begin at or before `begin`
@@ -528,7 +538,7 @@ __global__ void __launch_bounds__(kPagedThreads) paged_kernel(const __grid_const
       const uint32_t dst = s_ring + ld_stage * C::STEP_BYTES + row0 * W::ROW_BYTES;
       int id = seen ? page : -1;
       if (seen && (unsigned)page >= (unsigned)prm.pages) {   // not a page: flagged, its rows read as zeros
-        atomicCAS(prm.status, 0, CA_ERR_BAD_INDEX);
+        if (!prm.direct) atomicCAS(prm.status, 0, CA_ERR_BAD_INDEX);
         id = -1;
       }
       if (aligned && __all_sync(0xffffffffu, id >= 0 || lane >= W::KEYS)) {
@@ -627,6 +637,24 @@ __global__ void __launch_bounds__(kPagedThreads) paged_kernel(const __grid_const
   }
   let_next_start();
   cp_async_wait<0>();
+  if (prm.direct && blockIdx.x == 0) {
+    // This CTA looks at every index of the call and alone writes the status word, so that nothing has to clear it first.
+    int bad = 0;
+    for (int b = threadIdx.x; b < prm.batch; b += kPagedThreads) {
+      const long long rows = (long long)prm.lengths[b] + prm.appended;
+      bad |= rows < 0 || rows > (long long)prm.pages_per_sequence * prm.page_rows;
+    }
+    const unsigned entries = (unsigned)prm.batch * (unsigned)prm.pages_per_sequence;      // (few: kDirectRows of each sequence)
+#pragma unroll 4
+    for (unsigned e = threadIdx.x; e < entries; e += kPagedThreads) {
+      const int b = (int)(e / (unsigned)prm.pages_per_sequence), first = (int)(e % (unsigned)prm.pages_per_sequence) * prm.page_rows;
+      const Span s(prm, b, C::U);
+      const bool read = first < s.n && (first + prm.page_rows > s.lo || first < s.sink_end);
+      if (read) bad |= (unsigned)prm.page_table[e] >= (unsigned)prm.pages;
+    }
+    bad = __syncthreads_or(bad);
+    if (threadIdx.x == 0) *prm.status = bad ? CA_ERR_BAD_INDEX : CA_OK;
+  }
 }
 
 // Results of the parts that share a (sequence, key head, row tile) into one, in the order of the rows, whichever was
@@ -735,13 +763,20 @@ static int launch_paged_d(PagedParams& prm, LaunchStream st) {
   const int smem = C::smem(prm.group);
   auto kernel = paged_kernel<W, D>;
   CA_RETURN_IF_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+  const long long pairs = (long long)prm.batch * prm.heads_kv * prm.row_tiles;
+  prm.direct = (long long)prm.pages_per_sequence * prm.page_rows <= kDirectRows;
+  if (prm.direct) {
+    launch_chained(kernel, (unsigned)pairs, kPagedThreads, smem, st, prm);
+    CA_LAUNCH_CHECK();
+    return CA_OK;
+  }
   launch_chained(paged_plan_kernel, 1, 1024, 0, st, prm, C::U);
   CA_LAUNCH_CHECK();
   const int per_sm = min(4, (228 * 1024) / (smem + 1024));
   const int ctas = min(kPagedMaxCtas, sms * per_sm);
   launch_chained(kernel, ctas, kPagedThreads, smem, st, prm);
   CA_LAUNCH_CHECK();
-  const long long joins = (long long)prm.batch * prm.heads_kv * prm.row_tiles * ceil_div(min(prm.group, W::ROWS), kJoinRows);
+  const long long joins = pairs * ceil_div(min(prm.group, W::ROWS), kJoinRows);
   launch_chained(paged_join_kernel<W, D>, (unsigned)joins, kJoinThreads, 0, st, prm, ctas);
   CA_LAUNCH_CHECK();
   return CA_OK;

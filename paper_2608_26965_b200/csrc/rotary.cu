@@ -10,6 +10,7 @@
 // What bounds it: memory.  Every element is read and written once in 16-byte vectors; a thread keeps the sines
 // and cosines of its channels and goes through heads with them, which share the positions of a row.
 #include <math.h>
+#include <string.h>
 
 #include <type_traits>
 
@@ -207,9 +208,11 @@ __global__ void __launch_bounds__(256) rotary_kernel(const __grid_constant__ Rot
 // fraction is right to its last bit up to 2^32 radians per step.
 static unsigned long long turn_fraction(double freq) {
   constexpr unsigned long long kHi = 0x28BE60DB9391054Aull, kLo = 0x7F09D5F47D4D3770ull;   // 2^128 / (2 pi)
-  int exponent = 0;
-  const double m = frexp(fabs(freq), &exponent);
-  const unsigned long long M = (unsigned long long)ldexp(m, 53);
+  unsigned long long bits;
+  memcpy(&bits, &freq, sizeof(bits));
+  const int field = (int)(bits >> 52) & 0x7ff;
+  const unsigned long long M = (bits & 0xfffffffffffffULL) | (field ? 1ULL << 52 : 0);   // |freq| = M 2^(exponent - 53)
+  const int exponent = (field ? field : 1) - 1022;
   const unsigned __int128 low = (unsigned __int128)M * kLo, high = (unsigned __int128)M * kHi + (low >> 64);
   // the product is (high, low's lower word) 2^(exponent - 53 - 128) turns; word `shift` bits up is the fraction
   const unsigned long long w[4] = {(unsigned long long)low, (unsigned long long)high, (unsigned long long)(high >> 64), 0ull};

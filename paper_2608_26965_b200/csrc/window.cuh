@@ -14,7 +14,7 @@ struct WindowParams {
   int32_t* pieces;                  // [batch + 1] blocks of kWindowBlock rows of the batch items before
   int32_t* redo;                    // [batch * heads_q][blocks of kWindowBlock rows][16]: 16 rows each, to be computed again (null: all)
   int batch, heads_q, heads_kv, group, n_q, n_k, left, right, sinks;
-  int one_each;                     // no lengths, and a CTA of the tensor-core kernel for every block of rows: nothing is prepared for it
+  int one_each;                     // a CTA of the tensor-core kernel for every block of rows: nothing is prepared for it, marks are looked at one by one
   float scale_log2;
 };
 
@@ -68,9 +68,17 @@ struct WindowRow {
   __device__ __forceinline__ bool sees(int j) const { return j < end && (j >= from || j < sinks); }
 };
 
-// The tensor-core kernels want window_prepare before them (pieces, counters and status; the bf16 kernel sees to it), and window_ref
-// behind them, with `redo` set, for the rows that they marked.
-int launch_window_prepare(const WindowParams& prm, LaunchStream st);
+// Lengths looked at, by the threads of one block, which alone writes the status word.
+__device__ __forceinline__ void window_status(const WindowParams& prm, int threads) {
+  int bad = 0;
+  for (int i = threadIdx.x; i < prm.batch; i += threads)
+    bad |= (prm.len_q && (unsigned)prm.len_q[i] > (unsigned)prm.n_q) || (prm.len_k && (unsigned)prm.len_k[i] > (unsigned)prm.n_k);
+  bad = __syncthreads_or(bad);
+  if (threadIdx.x == 0) *prm.status = bad ? CA_ERR_BAD_INDEX : CA_OK;
+}
+
+// window_ref, with `redo` set, belongs behind the tensor-core kernels, for the rows that they marked.
+int launch_window_prepare(const WindowParams& prm, LaunchStream st);     // (the bf16 kernel's: pieces, counters, status)
 int launch_window_f32(const WindowParams& prm, int D, LaunchStream st);
 int launch_window_ref(const WindowParams& prm, int D, int dtype, LaunchStream st);
 int launch_window_tc(WindowParams& prm, int D, LaunchStream st);    // CA_ERR_UNSUPPORTED: strides that it does not take

@@ -60,6 +60,7 @@ __global__ void __launch_bounds__(kWfThreads) window_f32_kernel(const __grid_con
   using C = WfCfg<D>;
   extern __shared__ __align__(16) float smf[];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t4 = lane & 3;
+  if (blockIdx.x == 0) window_status(prm, kWfThreads);
   const int blocks = (prm.n_q + kWfRows - 1) / kWfRows;
   // (the last rows of a causal sequence see most: first)
   const int r0 = (blocks - 1 - (int)(blockIdx.x % blocks)) * kWfRows, bh = blockIdx.x / blocks, b = bh / prm.heads_q, h = bh % prm.heads_q;
@@ -224,7 +225,6 @@ __global__ void __launch_bounds__(kWfThreads) window_f32_kernel(const __grid_con
   if (lane == 0) {
     const int first = r0 + warp * 16;
     if (first < prm.n_q) prm.redo[((size_t)bh * ((prm.n_q + kWindowBlock - 1) / kWindowBlock) + first / kWindowBlock) * 16 + first % kWindowBlock / 16] = again ? 1 : 0;
-    if (again) atomicExch(prm.status + kRedoWord, 1);
   }
 }
 

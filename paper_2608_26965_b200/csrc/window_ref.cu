@@ -61,18 +61,26 @@ __global__ void __launch_bounds__(WrCfg<D, M>::THREADS) window_ref_kernel(const 
   float* sq = smf;
   float* sp = smf + C::OFF_P;
   const int tid = threadIdx.x, ty = tid >> 3, tx = tid & 7;
-  if (prm.redo) {
-    if (!prm.one_each && prm.status[kRedoWord] == 0) return;
-  } else if (blockIdx.x == 0) {
-    // the only one that writes the status word
-    int bad = 0;
-    for (int i = tid; i < prm.batch; i += C::THREADS)
-      bad |= (prm.len_q && (unsigned)prm.len_q[i] > (unsigned)prm.n_q) || (prm.len_k && (unsigned)prm.len_k[i] > (unsigned)prm.n_k);
-    bad = __syncthreads_or(bad);
-    if (tid == 0) *prm.status = bad ? CA_ERR_BAD_INDEX : CA_OK;
-  }
   const int blocks = (prm.n_q + M - 1) / M;
   const long long n_work = (long long)blocks * prm.heads_q * prm.batch;
+  auto marked = [&](int bh, int r0, int part, int len_q) {         // rows r0 + 16 part .. of a tile
+    const int r = r0 + 16 * part;
+    return r < len_q && prm.redo[((size_t)bh * ((prm.n_q + kWindowBlock - 1) / kWindowBlock) + r / kWindowBlock) * 16 + r % kWindowBlock / 16] != 0;
+  };
+  if (prm.redo) {
+    // hardly ever anything: all marks of this CTA's tiles at once
+    if (!prm.one_each && prm.status[kRedoWord] == 0) return;
+    int any = 0;
+    for (long long i = tid;; i += C::THREADS) {
+      const long long idx = blockIdx.x + i / (M / 16) * gridDim.x;
+      if (idx >= n_work) break;
+      const int bh = (int)(idx / blocks), r0 = (blocks - 1 - (int)(idx % blocks)) * M;
+      any |= marked(bh, r0, (int)(i % (M / 16)), WindowItem(prm, bh / prm.heads_q).len_q);
+    }
+    if (!__syncthreads_or(any)) return;
+  } else if (blockIdx.x == 0) {
+    window_status(prm, C::THREADS);
+  }
 #pragma unroll 1
   for (long long idx = blockIdx.x; idx < n_work; idx += gridDim.x) {
     // (the last rows of a causal sequence see most: first)
@@ -80,11 +88,10 @@ __global__ void __launch_bounds__(WrCfg<D, M>::THREADS) window_ref_kernel(const 
     const WindowItem it(prm, b);
     if (r0 >= it.len_q) continue;
     if (prm.redo) {
-      const int32_t* marks = prm.redo + ((size_t)bh * ((prm.n_q + kWindowBlock - 1) / kWindowBlock) + r0 / kWindowBlock) * 16 + r0 % kWindowBlock / 16;
-      int any = 0;
+      bool any = false;
 #pragma unroll
-      for (int i = 0; i < M / 16; ++i) any |= r0 + 16 * i < it.len_q ? marks[i] : 0;
-      if (any == 0) continue;
+      for (int i = 0; i < M / 16; ++i) any = any || marked(bh, r0, i, it.len_q);
+      if (!any) continue;
     }
     const int rows = min(M, it.len_q - r0);
     const WindowSpan span(prm, it, r0, r0 + rows, kWrKeys);
@@ -227,8 +234,8 @@ static int launch_window_ref_m(const WindowParams& prm, LaunchStream st) {
   auto kernel = window_ref_kernel<T, D, M>;
   CA_RETURN_IF_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM));
   const long long n_work = (long long)ceil_div(prm.n_q, M) * prm.heads_q * prm.batch;
-  // a CTA for every tile of rows; to compute rows again, hardly ever any, as many as are on the GPU at a time
-  const long long most = prm.redo ? 296 : 0x7fffffffLL;
+  // a CTA for every tile of rows; to compute rows again, hardly ever any, one to an SM
+  const long long most = prm.redo ? 148 : 0x7fffffffLL;
   launch_chained(kernel, (unsigned)(n_work < most ? n_work : most), C::THREADS, C::SMEM, st, prm);
   CA_LAUNCH_CHECK();
   return CA_OK;
@@ -317,11 +324,12 @@ int launch_window(const ca_window_t& p, const ca_rows_t* Q, const ca_rows_t* K, 
     if (p.dtype == CA_DTYPE_BF16) {
       rc = launch_window_tc(prm, p.head_dim, st);
     } else {
-      rc = launch_window_prepare(prm, st);
-      if (rc == CA_OK) rc = launch_window_f32(prm, p.head_dim, st);
+      prm.one_each = 1;
+      rc = launch_window_f32(prm, p.head_dim, st);
     }
     if (rc == CA_OK) return launch_window_ref(prm, p.head_dim, p.dtype, st);
     if (rc != CA_ERR_UNSUPPORTED) return rc;
+    prm.one_each = 0;
     prm.redo = nullptr;                         // strides of a broadcast, or too many pieces: on the CUDA cores
   }
   return launch_window_ref(prm, p.head_dim, p.dtype, st);

@@ -150,6 +150,7 @@ window_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
   const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
   const int sinks = prm.w.sinks;
 
+  if (prm.w.one_each && blockIdx.x == 0) window_status(prm.w, kWtThreads);     // (a wait that gives up writes it a second later)
   if (tid == 0) {
     for (int i = 0; i < 2; ++i) {
       mbar_init(b_q_full(i), 1);
@@ -192,7 +193,6 @@ window_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
     // ---------------------------------------------------------- work
     if (lane == 0) {
       const int all_blocks = prm.w.one_each ? prm.blocks * prm.w.batch : prm.w.pieces[prm.w.batch], n_work = all_blocks * prm.w.heads_q;
-      if (prm.w.one_each && blockIdx.x == 0) prm.w.status[0] = CA_OK;      // (a wait that gives up writes it a second later)
       int n = 0;
       for (int idx = blockIdx.x;; ++n) {
         // A piece is claimed when the one before is nearly loaded, not earlier: what a CTA has claimed another that is done cannot take
@@ -227,6 +227,10 @@ window_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
             w.r0 = (block - prm.w.pieces[lo]) * kWtRows;
           }
           const WindowItem it(prm.w, w.b);
+          if (w.r0 >= it.len_q) {                        // (of one_each: a block behind its sequence)
+            w.b = -1;
+            idx = n_work;
+          }
           w.len_q = it.len_q;
           w.len_k = it.len_k;
           const WindowSpan all(prm.w, it, w.r0, min(w.r0 + kWtRows, it.len_q), kWtKeys);
@@ -720,9 +724,8 @@ int launch_window_tc(WindowParams& w, int D, LaunchStream st) {
              (w.n_q == 1 || w.o_n % 16 == 0);
   const int sms = multiprocessors();
   if (sms == 0) return CA_ERR_CUDA;
-  // A CTA for every piece, and no lengths: no counter, no list of pieces, and the marks are few enough to be looked at one by one; a
-  // launch less.
-  prm.w.one_each = w.one_each = !w.len_q && !w.len_k && n_work <= sms;
+  // A CTA for every piece: no counter, no list of pieces, and the marks are few enough to be looked at one by one; a launch less.
+  prm.w.one_each = w.one_each = n_work <= sms;
   if (!w.one_each) {
     const int rc = launch_window_prepare(w, st);
     if (rc != CA_OK) return rc;

@@ -277,3 +277,43 @@ def test_pools_beyond_32_bits(dtype):
     O, lse = cache.paged_attention_fwd(q, appended=n)
     assert cache.last_status() == 0
     check(cache, q, [n], O, lse)
+
+
+def test_binding_refuses_what_does_not_fit():
+    cache, q = make(3, [40, 40], 4, 2, 64, "bf16", 16)
+    k = torch.zeros((2, 2, 3, 64), dtype=torch.bfloat16, device=DEV)
+    rot = binding.Rotary(64, [4])
+    pos = torch.zeros((2, 3, 1), dtype=torch.int32, device=DEV)
+    one = q[:1]
+    for bad in (q.float(), one, q.transpose(0, 1), q.cpu(), torch.zeros((2, 4, 1, 128), dtype=torch.bfloat16, device=DEV)[..., ::2], None):
+        with pytest.raises(binding.ClusterAttnError):
+            cache.paged_attention_fwd(bad)
+    with pytest.raises(binding.ClusterAttnError):
+        cache.paged_attention_fwd(q, out=q.float())
+    with pytest.raises(binding.ClusterAttnError):          # 16-byte alignment
+        cache.paged_attention_fwd(torch.zeros((2, 4, 1, 72), dtype=torch.bfloat16, device=DEV)[..., 1:65])
+    for args, kw in (((k, k[:, :, :2]), {}), ((k, k), dict(rotary=rot)), ((k, k), dict(positions=pos)), ((k, k), dict(rotary=rot, positions=pos.long())),
+                     ((k, k), dict(rotary=rot, positions=pos[:, :2])), ((k, k), dict(rotary=binding.Rotary(128, [4]), positions=pos)),
+                     ((k, k), dict(count=torch.zeros(3, dtype=torch.int32, device=DEV))), ((k[:, :, :0], k[:, :, :0]), {}), ((k.float(), k.float()), {})):
+        with pytest.raises(binding.ClusterAttnError):
+            cache.cache_append(*args, **kw)
+    with pytest.raises(AttributeError):
+        cache.lengths = torch.zeros(2, dtype=torch.int32, device=DEV)
+    p = cache.problem
+    for kw in (dict(lengths=torch.zeros(3, dtype=torch.int32, device=DEV)), dict(page_table=torch.zeros((2, 1), dtype=torch.int64, device=DEV)),
+               dict(K_pages=torch.zeros((1, 2, 16, 64), dtype=torch.bfloat16, device=DEV))):
+        with pytest.raises(binding.ClusterAttnError):
+            binding.PagedCache(p, DEV, **kw)
+    for bad_q, bad_k, bad_pos in ((q.half(), None, pos), (k, k.float(), pos), (k, k[:1], pos), (k, k, pos[:, :, :0]), (k, k, pos.cpu()), (k, k, None), (k[..., :32], None, pos)):
+        with pytest.raises(binding.ClusterAttnError):
+            binding.rotary_axes(rot, bad_q, bad_k, bad_pos)
+    with pytest.raises(binding.ClusterAttnError):
+        binding.rotary_axes(rot, k, None, pos, out_k=k)
+    w = binding.WindowPlan(binding.make_window_problem(2, 4, 2, 3, 3, 64, "bf16", 1, 0), DEV)
+    q3 = torch.zeros((2, 4, 3, 64), dtype=torch.bfloat16, device=DEV)
+    for args, kw in (((q3, k, k.float()), {}), ((k, k, k), {}), ((q3, k, k), dict(len_q=torch.zeros(2, device=DEV))), ((q3, k, k), dict(out=q3[:, :, :2]))):
+        with pytest.raises(binding.ClusterAttnError):
+            w.window_attention_fwd(*args, **kw)
+    side = torch.cuda.Stream()
+    assert cache.paged_attention_fwd(q, stream=side)[0] is cache.O
+    torch.cuda.synchronize()
