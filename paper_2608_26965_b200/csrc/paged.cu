@@ -35,6 +35,7 @@ constexpr int kPagedThreads = kPagedWarps * 32;
 constexpr int kPairUnits = 3;
 // Caches of at most so many rows a sequence are not split: a CTA for every (sequence, key head, row tile), one launch instead of three.
 constexpr int kDirectRows = 256;
+constexpr int kAddUp = 256;                    // sequences whose lengths every CTA adds up by itself; of more, a launch does
 constexpr int kPagedMaxCtas = 640;           // most CTAs of a launch: the workspace holds two partial results of each
 
 __host__ __device__ inline int ceil_div_device(int a, int b) { return (a + b - 1) / b; }
@@ -48,9 +49,11 @@ struct PagedParams {
   const void *k_pages, *v_pages;
   const int32_t *lengths, *page_table;
   int* status;
-  long long* units;              // [batch + 1] units of a (key head, row tile) of the sequences before
+  long long* units;              // [batch + 1] units of a (key head, row tile) of the sequences before (planned calls)
+  int* bad;                      // [CTAs] whether a CTA met a page that is none
   float* partial;                // [2 * CTAs] O [rows][D] (not divided), {m (log2 units), l} [rows]; rows (D + 4) floats apart
   int batch, heads_q, heads_kv, group, row_tiles, page_rows, pages, pages_per_sequence, appended, left, sinks;
+  int planned;                   // units come from paged_plan_kernel, otherwise every CTA adds up the lengths itself
   int direct;                    // a CTA for every (sequence, key head, row tile): nothing is planned or joined
   float scale_log2;
 };
@@ -71,24 +74,19 @@ struct Span {
   __device__ __forceinline__ bool sees(int j) const { return j < n && (j >= lo || j < sink_end); }
 };
 
-// One CTA: units before each sequence, status cleared, lengths looked at.
+// One CTA: units before each sequence.
 __global__ void __launch_bounds__(1024) paged_plan_kernel(const __grid_constant__ PagedParams prm, int U) {
   wait_for_previous();
   let_next_start();
   __shared__ long long warp_sum[32];
   __shared__ long long carry;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  int bad = 0;
   if (tid == 0) { carry = 0; prm.units[0] = 0; }
   __syncthreads();
   for (int base = 0; base < prm.batch; base += blockDim.x) {
     const int b = base + tid;
     long long v = 0;
-    if (b < prm.batch) {
-      const long long rows = (long long)prm.lengths[b] + prm.appended;
-      bad |= rows < 0 || rows > (long long)prm.pages_per_sequence * prm.page_rows;
-      v = Span(prm, b, U).tiles + kPairUnits;
-    }
+    if (b < prm.batch) v = Span(prm, b, U).tiles + kPairUnits;
     for (int d = 1; d < 32; d <<= 1) {
       const long long o = __shfl_up_sync(0xffffffffu, v, d);
       if (lane >= d) v += o;
@@ -102,8 +100,43 @@ __global__ void __launch_bounds__(1024) paged_plan_kernel(const __grid_constant_
     if (tid == (int)blockDim.x - 1) carry = before + v;
     __syncthreads();
   }
-  bad = __syncthreads_or(bad);
-  if (tid == 0) *prm.status = bad ? CA_ERR_BAD_INDEX : CA_OK;
+}
+
+template <int THREADS>
+__device__ __forceinline__ int bad_lengths(const PagedParams& prm) {
+  int bad = 0;
+  for (int b = threadIdx.x; b < prm.batch; b += THREADS) {
+    const long long rows = (long long)prm.lengths[b] + prm.appended;
+    bad |= rows < 0 || rows > (long long)prm.pages_per_sequence * prm.page_rows;
+  }
+  return bad;
+}
+
+// Units of all sequences, of those before sequence `b`, and of it, added up by the THREADS threads of a CTA.
+struct Units {
+  long long total, before;
+  int own;
+};
+template <int THREADS>
+__device__ __forceinline__ Units add_units(const PagedParams& prm, int b, int U) {
+  __shared__ long long part[THREADS / 32][2];
+  long long all = 0, before = 0;
+  for (int i = threadIdx.x; i < prm.batch; i += THREADS) {
+    const int v = Span(prm, i, U).tiles + kPairUnits;
+    all += v;
+    if (i < b) before += v;
+  }
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) {
+    all += __shfl_xor_sync(0xffffffffu, all, d);
+    before += __shfl_xor_sync(0xffffffffu, before, d);
+  }
+  if ((threadIdx.x & 31) == 0) { part[threadIdx.x >> 5][0] = all; part[threadIdx.x >> 5][1] = before; }
+  __syncthreads();
+  Units r{0, 0, Span(prm, b, U).tiles + kPairUnits};
+#pragma unroll
+  for (int w = 0; w < THREADS / 32; ++w) { r.total += part[w][0]; r.before += part[w][1]; }
+  return r;
 }
 
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool in) {
@@ -447,6 +480,14 @@ struct Place {
     last = (int)max(0LL, behind);
     pos = base + kPairUnits + tiles;
   }
+  // position `begin` in sequence `seq`, which begins at `base` and has `each` units per (key head, row tile)
+  __device__ __forceinline__ void place(int seq, long long base, int each, int row_tiles, long long begin) {
+    const int pair = (int)((begin - base) / each);
+    b = seq;
+    h = pair / row_tiles;
+    rt = pair % row_tiles;
+    cut(base + (long long)pair * each, begin, each - kPairUnits);
+  }
   // the next one; `span` follows the sequence
   __device__ __forceinline__ void next(const PagedParams& prm, Span& span, int U) {
     tile = last = 0;
@@ -481,6 +522,11 @@ __global__ void __launch_bounds__(kPagedThreads) paged_kernel(const __grid_const
   wait_for_previous();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int per = prm.heads_kv * prm.row_tiles;              // (key head, row tile) pairs of a sequence
+  auto no_part = [&]() {
+    if (threadIdx.x == 0) prm.bad[blockIdx.x] = 0;
+    let_next_start();
+  };
+  int bad = 0;
   Place at;
   if (prm.direct) {
     at.b = blockIdx.x / per;
@@ -489,10 +535,10 @@ __global__ void __launch_bounds__(kPagedThreads) paged_kernel(const __grid_const
     at.pos = at.end = 0;                                     // (none behind it)
     at.tile = 0;
     at.last = Span(prm, at.b, C::U).tiles;
-  } else {
+  } else if (prm.planned) {
     const long long total = prm.units[prm.batch] * per;
     const long long parts = min((long long)gridDim.x, total);
-    if (blockIdx.x >= parts) { let_next_start(); return; }
+    if (blockIdx.x >= parts) { no_part(); return; }
     const long long begin = total * blockIdx.x / parts;
     at.end = total * (blockIdx.x + 1) / parts;
     int lo = 0, hi = prm.batch - 1;                          // last sequence whose units begin at or before `begin`
@@ -501,13 +547,38 @@ __global__ void __launch_bounds__(kPagedThreads) paged_kernel(const __grid_const
       if (prm.units[mid] * per <= begin) lo = mid;
       else hi = mid - 1;
     }
-    const long long off = begin - prm.units[lo] * per;
-    const int each = (int)(prm.units[lo + 1] - prm.units[lo]);
-    const int pair = (int)(off / each);
-    at.b = lo;
-    at.h = pair / prm.row_tiles;
-    at.rt = pair % prm.row_tiles;
-    at.cut(prm.units[lo] * per + (long long)pair * each, begin, each - kPairUnits);
+    at.place(lo, prm.units[lo] * per, (int)(prm.units[lo + 1] - prm.units[lo]), prm.row_tiles, begin);
+  } else {
+    // Every CTA adds up the lengths by itself: thread t has sequences 2 t and 2 t + 1.
+    static_assert(kAddUp == 2 * kPagedThreads, "two sequences to a thread");
+    long long* sums = reinterpret_cast<long long*>(smem);    // (the rings are not in use yet) [4] of warps, then what is found
+    const int b0 = 2 * (int)threadIdx.x;
+    const int v0 = b0 < prm.batch ? Span(prm, b0, C::U).tiles + kPairUnits : 0, v1 = b0 + 1 < prm.batch ? Span(prm, b0 + 1, C::U).tiles + kPairUnits : 0;
+    long long behind = (long long)v0 + v1;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const long long o = __shfl_up_sync(0xffffffffu, behind, d);
+      if (lane >= d) behind += o;
+    }
+    if (lane == 31) sums[warp] = behind;
+    __syncthreads();
+    long long total = 0;
+#pragma unroll
+    for (int w = 0; w < kPagedWarps; ++w) {
+      if (w < warp) behind += sums[w];
+      total += sums[w];
+    }
+    total *= per;
+    const long long parts = min((long long)gridDim.x, total);
+    if (blockIdx.x >= parts) { no_part(); return; }
+    const long long begin = total * blockIdx.x / parts;
+    at.end = total * (blockIdx.x + 1) / parts;
+    const long long base1 = (behind - v1) * per, base0 = base1 - (long long)v0 * per;
+    if (v0 && begin >= base0 && begin < base1) { sums[4] = b0; sums[5] = base0; sums[6] = v0; }
+    if (v1 && begin >= base1 && begin < behind * per) { sums[4] = b0 + 1; sums[5] = base1; sums[6] = v1; }
+    __syncthreads();
+    at.place((int)sums[4], sums[5], (int)sums[6], prm.row_tiles, begin);
+    __syncthreads();                                         // (read before the rings are filled)
   }
   Span span(prm, at.b, C::U);
   if (!at.there()) at.next(prm, span, C::U);
@@ -538,7 +609,7 @@ __global__ void __launch_bounds__(kPagedThreads) paged_kernel(const __grid_const
       const uint32_t dst = s_ring + ld_stage * C::STEP_BYTES + row0 * W::ROW_BYTES;
       int id = seen ? page : -1;
       if (seen && (unsigned)page >= (unsigned)prm.pages) {   // not a page: flagged, its rows read as zeros
-        if (!prm.direct) atomicCAS(prm.status, 0, CA_ERR_BAD_INDEX);
+        bad = 1;
         id = -1;
       }
       if (aligned && __all_sync(0xffffffffu, id >= 0 || lane >= W::KEYS)) {
@@ -637,13 +708,12 @@ __global__ void __launch_bounds__(kPagedThreads) paged_kernel(const __grid_const
   }
   let_next_start();
   cp_async_wait<0>();
-  if (prm.direct && blockIdx.x == 0) {
+  if (!prm.direct) {
+    bad = __syncthreads_or(bad);
+    if (threadIdx.x == 0) prm.bad[blockIdx.x] = bad;         // (the launch that joins makes the status of it)
+  } else if (blockIdx.x == 0) {
     // This CTA looks at every index of the call and alone writes the status word, so that nothing has to clear it first.
-    int bad = 0;
-    for (int b = threadIdx.x; b < prm.batch; b += kPagedThreads) {
-      const long long rows = (long long)prm.lengths[b] + prm.appended;
-      bad |= rows < 0 || rows > (long long)prm.pages_per_sequence * prm.page_rows;
-    }
+    bad = bad_lengths<kPagedThreads>(prm);
     const unsigned entries = (unsigned)prm.batch * (unsigned)prm.pages_per_sequence;      // (few: kDirectRows of each sequence)
 #pragma unroll 4
     for (unsigned e = threadIdx.x; e < entries; e += kPagedThreads) {
@@ -669,9 +739,19 @@ __global__ void __launch_bounds__(kJoinThreads) paged_join_kernel(const __grid_c
   const int chunks = ceil_div_device(min(prm.group, W::ROWS), kJoinRows);
   const int chunk = blockIdx.x % chunks, pair = blockIdx.x / chunks, per = prm.heads_kv * prm.row_tiles;
   const int b = pair / per, h = pair % per / prm.row_tiles, rt = pair % prm.row_tiles;
-  const long long total = prm.units[prm.batch] * per, parts = min((long long)ctas, total);
-  const int each = (int)(prm.units[b + 1] - prm.units[b]);
-  const long long base = prm.units[b] * per + (long long)(pair % per) * each;
+  if (blockIdx.x == 0) {
+    // the status: this CTA alone writes it
+    int bad = bad_lengths<kJoinThreads>(prm);
+    for (int c = threadIdx.x; c < ctas; c += kJoinThreads) bad |= prm.bad[c];
+    bad = __syncthreads_or(bad);
+    if (threadIdx.x == 0) *prm.status = bad ? CA_ERR_BAD_INDEX : CA_OK;
+  }
+  Units u;
+  if (prm.planned) u = Units{prm.units[prm.batch], prm.units[b], (int)(prm.units[b + 1] - prm.units[b])};
+  else u = add_units<kJoinThreads>(prm, b, C::U);
+  const int each = u.own;
+  const long long total = u.total * per, parts = min((long long)ctas, total);
+  const long long base = u.before * per + (long long)(pair % per) * each;
   const int cta0 = part_of(base + kPairUnits, parts, total), cta1 = part_of(base + each - 1, parts, total);
   const int row0 = chunk * kJoinRows, rows = min(min(prm.group - rt * W::ROWS, W::ROWS) - row0, kJoinRows);
   if (cta0 == cta1 || rows <= 0) return;
@@ -739,6 +819,7 @@ static int row_tile(const ca_cache_t& c) {
 struct PagedWs {
   int* status;
   long long* units;
+  int* bad;
   float* partial;
   size_t bytes;
 };
@@ -748,6 +829,7 @@ static PagedWs carve_paged(const ca_cache_t& c, void* base) {
   const int rows = row_tile(c);
   w.status = k.take<int>(kStatusBytes / sizeof(int));
   w.units = k.take<long long>((size_t)c.batch + 1);
+  w.bad = k.take<int>(kPagedMaxCtas);
   w.partial = k.take<float>((size_t)2 * kPagedMaxCtas * rows * (c.head_dim + 4));
   w.bytes = k.used();
   return w;
@@ -770,8 +852,11 @@ static int launch_paged_d(PagedParams& prm, LaunchStream st) {
     CA_LAUNCH_CHECK();
     return CA_OK;
   }
-  launch_chained(paged_plan_kernel, 1, 1024, 0, st, prm, C::U);
-  CA_LAUNCH_CHECK();
+  prm.planned = prm.batch > kAddUp;
+  if (prm.planned) {
+    launch_chained(paged_plan_kernel, 1, 1024, 0, st, prm, C::U);
+    CA_LAUNCH_CHECK();
+  }
   const int per_sm = min(4, (228 * 1024) / (smem + 1024));
   const int ctas = min(kPagedMaxCtas, sms * per_sm);
   launch_chained(kernel, ctas, kPagedThreads, smem, st, prm);
@@ -791,7 +876,7 @@ int launch_paged(const ca_cache_t& c, const ca_rows_t* Q, const void* K_pages, c
   prm.lse = lse;
   prm.k_pages = K_pages; prm.v_pages = V_pages;
   prm.lengths = lengths; prm.page_table = page_table;
-  prm.status = w.status; prm.units = w.units; prm.partial = w.partial;
+  prm.status = w.status; prm.units = w.units; prm.bad = w.bad; prm.partial = w.partial;
   prm.batch = c.batch; prm.heads_q = c.heads_q; prm.heads_kv = c.heads_kv; prm.group = c.heads_q / c.heads_kv;
   prm.page_rows = c.page_rows; prm.pages = c.pages; prm.pages_per_sequence = c.pages_per_sequence;
   prm.appended = appended; prm.left = c.left; prm.sinks = c.sinks;

@@ -81,10 +81,13 @@ def test_long_rows_are_split_and_joined(dtype, d, lengths, left, sinks):
         assert torch.equal(O, first[0]) and torch.equal(lse, first[1])
 
 
-def test_more_sequences_than_threads_of_the_plan():
+@pytest.mark.parametrize("spare", [0, 20])
+def test_more_sequences_than_threads_of_the_plan(spare):
+    """Of a table of few rows (a CTA for each sequence and head) and of many (units added up by a launch of its own)."""
     lengths = [(7 * i) % 41 for i in range(2500)]
-    cache, q = make(1, lengths, 2, 2, 64, "bf16", 16)
+    cache, q = make(1, lengths, 2, 2, 64, "bf16", 16, spare=spare)
     O, lse = cache.paged_attention_fwd(q)
+    assert cache.last_status() == 0
     check(cache, q, lengths[:60], O, lse)
     for at in (1023, 1024, 1025, 2047, 2048, 2499):
         n = lengths[at]
@@ -92,6 +95,21 @@ def test_more_sequences_than_threads_of_the_plan():
         want, l64, bound, lb, empty = ref.attend(q[at, 1].double(), k, v, torch.ones((1, n), dtype=torch.bool, device=DEV), 1 / 8, cache.dtype, False)
         ref.check(O[at, 1], want, bound, f"sequence {at}")
         ref.check_lse(lse[at, 1].double(), l64, lb, empty, f"sequence {at}")
+
+
+@pytest.mark.parametrize("batch", [1, 2, 127, 128, 129, 255, 256, 257, 300])
+def test_batches_around_the_threads_of_a_cta(batch):
+    g = torch.Generator()
+    g.manual_seed(batch)
+    lengths = [int(x) for x in torch.randint(0, 500, (batch,), generator=g)]
+    lengths[-1] = 700
+    cache, q = make(batch, lengths, 4, 2, 64, "bf16", 16, left=300, sinks=5)
+    O, lse = cache.paged_attention_fwd(q)
+    assert cache.last_status() == 0
+    check(cache, q, lengths, O, lse)
+    cache.page_table[batch - 1, 40] = cache.problem.pages
+    cache.paged_attention_fwd(q)
+    assert cache.last_status() == binding.CA_ERR_BAD_INDEX
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
@@ -119,8 +137,9 @@ def test_rows_that_are_not_numbers_where_they_are_seen():
     assert torch.isinf(O[1].float()).all() and torch.isnan(O[2].float()).all() and torch.isnan(lse[2]).all()
 
 
-def test_bad_pages_and_lengths_are_recorded():
-    cache, q = make(5, [40, 40], 2, 1, 64, "bf16", 16, garbage=False)
+@pytest.mark.parametrize("spare", [0, 20])
+def test_bad_pages_and_lengths_are_recorded(spare):
+    cache, q = make(5, [40, 40], 2, 1, 64, "bf16", 16, garbage=False, spare=spare)
     good = cache.paged_attention_fwd(q)[0].clone()
     kept = cache.page_table[1, 1].clone()
     for bad in (cache.problem.pages, -1, 2 ** 31 - 1, -2 ** 31):
@@ -134,7 +153,7 @@ def test_bad_pages_and_lengths_are_recorded():
     assert cache.last_status() == binding.CA_ERR_BAD_INDEX
     assert (O[0] == 0).all() and torch.isinf(lse[0]).all() and torch.equal(O[1], good[1])
     cache.lengths[0] = 2 ** 31 - 1
-    O, lse = cache.paged_attention_fwd(q, appended=2 ** 31 - 1)             # both sequences: cut to the table's 48 rows
+    O, lse = cache.paged_attention_fwd(q, appended=2 ** 31 - 1)             # both sequences: cut to the table's rows
     assert cache.last_status() == binding.CA_ERR_BAD_INDEX
     cache.lengths.fill_(40)
     assert torch.equal(cache.paged_attention_fwd(q)[0], good) and cache.last_status() == 0
