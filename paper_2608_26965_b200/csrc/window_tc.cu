@@ -4,7 +4,7 @@
 // value tiles of 128 rows that they see: the first tokens' tiles, then the window's.  For each of the two and every key tile
 //     S  = Q K^T           tcgen05.mma, Q and K in shared memory
 //     P  = exp2(S c - m)   one query row per thread, so that its sum needs no other thread; P goes back over S in
-//                          tensor memory as bf16, and its first half is handed to the products before the second is computed
+//                          tensor memory as bf16, and its first three quarters are handed to the products before the last is computed
 //     O += P V             tcgen05.mma, P from tensor memory
 // and while four warps are at the softmax of one tile, the tensor core is at the products of the other.  Roles: warp 0 loads (TMA, 128-byte
 // swizzle), one thread of warp 1 issues the products, warp 2 sets value rows behind the last key to zero, warp 3 hands out work,
@@ -21,11 +21,12 @@
 // memory fed both operands of Q K^T without a pause (they need all of its 128 bytes a cycle, and the loads of the next tiles and V
 // come on top); the exponentials 1,900 of the special-function unit's time.  Between the two lies the chain S -> P -> O of each
 // query tile.  Calls in a row are bound by power: 40 heads of 32,760 rows, d = 128, two frames of 1,560 to either side and the first
-// one take 4.10 ms by themselves and 4.65 in a row (1.06 PFLOP/s of visible pairs, 1.18 with the masked parts of tiles; plain
+// one take 4.01 ms by themselves and 4.62 in a row (1.06 PFLOP/s of visible pairs, 1.19 with the masked parts of tiles; plain
 // products of 8,192^3 1.41 in a row).  Tried and slower: 16 softmax warps with half of a row's columns each (4.40 ms), the
 // issuing thread looking at barriers without a pause (5.27: its looks delay everybody's), a pass for the exact maximum (4.17),
 // every eighth instead of every sixteenth pair of exponentials on the FMA units (4.26; none 4.09, but 476 us instead of 452 at d = 64,
-// 8 heads of 18,944 rows).
+// 8 heads of 18,944 rows), P handed over in halves (4.07) or in whole (4.19), steps of 64 keys with two score buffers to a query tile
+// (6.42 in a row: the issuing thread is what they wait for).
 #include <math.h>
 
 #include "tc_ptx.cuh"
@@ -131,7 +132,7 @@ window_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
   auto b_q_full = [&](int i) { return bar0 + 8 * i; };
   auto b_q_empty = [&](int i) { return bar0 + 16 + 8 * i; };
   auto b_s_full = [&](int i) { return bar0 + 32 + 8 * i; };
-  auto b_p_half = [&](int i) { return bar0 + 48 + 8 * i; };
+  auto b_p_most = [&](int i) { return bar0 + 48 + 8 * i; };
   auto b_p_ready = [&](int i) { return bar0 + 64 + 8 * i; };
   auto b_pv_done = [&](int i) { return bar0 + 80 + 8 * i; };
   auto b_o_full = [&](int i) { return bar0 + 96 + 8 * i; };
@@ -156,7 +157,7 @@ window_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
       mbar_init(b_q_full(i), 1);
       mbar_init(b_q_empty(i), 1);
       mbar_init(b_s_full(i), 1);
-      mbar_init(b_p_half(i), 4);
+      mbar_init(b_p_most(i), 4);
       mbar_init(b_p_ready(i), 4);
       mbar_init(b_pv_done(i), 1);
       mbar_init(b_o_full(i), 1);
@@ -398,16 +399,16 @@ window_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
               if (n_o[i] > 0 && !wait(b_o_empty(i), n_o[i] - 1)) { ok = false; break; }
               ++n_o[i];
             }
-            if (!wait(b_p_half(i), n_pv[i])) { ok = false; break; }
+            if (!wait(b_p_most(i), n_pv[i])) { ok = false; break; }
             tc_fence_after();
             const uint64_t vd = v_desc0 + ((v_slot * C::TILE_BYTES) >> 4);
 #pragma unroll
-            for (int ks = 0; ks < 4; ++ks)
+            for (int ks = 0; ks < 6; ++ks)
               mma_ts(tmem_o(i), tmem_s(i) + ks * 8, vd + (uint64_t)(ks * (2048 >> 4)), idesc_pv, (ks > 0 || !was_first[i]) ? 1u : 0u);
             if (!wait(b_p_ready(i), n_pv[i])) { ok = false; break; }
             tc_fence_after();
 #pragma unroll
-            for (int ks = 4; ks < 8; ++ks)
+            for (int ks = 6; ks < 8; ++ks)
               mma_ts(tmem_o(i), tmem_s(i) + ks * 8, vd + (uint64_t)(ks * (2048 >> 4)), idesc_pv, 1u);
             ++n_pv[i];
           }
@@ -570,13 +571,13 @@ window_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
         tmem_wait_ld32(sb);
         tmem_ld32(t_s + 64, sa);
         exponentials(sb, 32);
-        tmem_wait_st();
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(b_p_half(i));             // the products of the first 64 keys need not wait for the others
         tmem_wait_ld32(sa);
         tmem_ld32(t_s + 96, sb);
         exponentials(sa, 64);
+        tmem_wait_st();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(b_p_most(i));             // the products of the first 96 keys need not wait for the others
         tmem_wait_ld32(sb);
         exponentials(sb, 96);
         tmem_wait_st();
