@@ -95,6 +95,10 @@ int launch_attn_ref(const ca_problem_t& pr, const void* Qp, const void* Kp, cons
                     float* lse, int* status, LaunchStream st, const int32_t* redo = nullptr, int redo_tiles = 0,
                     int* redo_count = nullptr);
 
+// Probabilities are summed 2^32 times smaller than they are: 2^31 of the largest finite values do not add up to infinity before the
+// division (an infinite sum that a new maximum then scales by zero would be a NaN).
+constexpr float kWeightScale = 0x1p-32f, kWeightBack = 0x1p32f;
+
 // rotary.cu
 int check_rows(const ca_rows_t* x, int batch, int heads, int n, int D, int dtype, bool written);
 int launch_rotary_axes(const ca_rotary_t& rot, int batch, int heads_q, int heads_k, int n, int D, int dtype, int inverse,

@@ -254,16 +254,17 @@ struct WarpMma {
           for (int i = 0; i < 4; ++i) o[t][n][i] *= by[i & 1];
       }
       // Probabilities in two bf16 parts, the upper bits and the rest: the products have time to spare, and the result the accuracy of
-      // fp32.  The rest is kept above zero, so that an infinite value stays one (of a weight that is 1 at least 1e-30 is nothing).
+      // fp32.  The rest is at least 2^-24 of the probability, half a step of fp32: where it is zero, 0 x infinity would make an infinite
+      // value a NaN, and of a weight that is itself zero it stays zero, however large the value.
       const float ref0 = m[t][0] == -INFINITY ? 0.f : -m[t][0], ref1 = m[t][1] == -INFINITY ? 0.f : -m[t][1];
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const float p0 = ex2_approx(fmaf(s[t][2 * h], scale, ref0)), p1 = ex2_approx(fmaf(s[t][2 * h + 1], scale, ref1));
+        const float p0 = ex2_approx(fmaf(s[t][2 * h], scale, ref0)) * kWeightScale, p1 = ex2_approx(fmaf(s[t][2 * h + 1], scale, ref1)) * kWeightScale;
         l[t][0] += p0;
         l[t][1] += p1;
         const uint32_t u0 = __float_as_uint(p0) & 0xffff0000u, u1 = __float_as_uint(p1) & 0xffff0000u;
         hi[t][h] = transpose8x8(__byte_perm(u0, u1, 0x7632));
-        lo[t][h] = transpose8x8(pack_bf16x2(fmaxf(p0 - __uint_as_float(u0), 1e-30f), fmaxf(p1 - __uint_as_float(u1), 1e-30f)));
+        lo[t][h] = transpose8x8(pack_bf16x2(fmaxf(p0 - __uint_as_float(u0), p0 * 0x1p-24f), fmaxf(p1 - __uint_as_float(u1), p1 * 0x1p-24f)));
       }
     }
 #pragma unroll
@@ -391,7 +392,7 @@ struct WarpFma {
     }
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-      p[r] = ex2_approx(s[r] - (m[r] == -INFINITY ? 0.f : m[r]));
+      p[r] = ex2_approx(s[r] - (m[r] == -INFINITY ? 0.f : m[r])) * kWeightScale;
       if (quarter == 0) l[r] += p[r];
     }
     if (quarter == 0) {
@@ -511,7 +512,7 @@ __device__ __forceinline__ void finish_row(const PagedParams& prm, int b, int he
   if (l == 0.f) o = make_float4(0.f, 0.f, 0.f, 0.f);
   else o = make_float4(o.x / l, o.y / l, o.z / l, o.w / l);
   store4(static_cast<T*>(prm.o) + b * prm.o_b + head * prm.o_h + col, o);
-  if (col == 0 && prm.lse) prm.lse[(size_t)b * prm.heads_q + head] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
+  if (col == 0 && prm.lse) prm.lse[(size_t)b * prm.heads_q + head] = l == 0.f ? -INFINITY : (m + log2f(l * kWeightBack)) * 0.6931471805599453f;
 }
 
 template <typename W, int D>

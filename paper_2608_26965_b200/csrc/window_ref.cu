@@ -174,7 +174,7 @@ __global__ void __launch_bounds__(WrCfg<D, M>::THREADS) window_ref_kernel(const 
         }
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          const float p = ex2_approx(s[j] - ref);
+          const float p = ex2_approx(s[j] - ref) * kWeightScale;
           if (seen[j]) l[i] += p;
           sp[(R * ty + i) * C::P_PITCH + tx + 8 * j] = seen[j] ? p : -1.f;      // (no probability: takes no part)
         }
@@ -223,7 +223,7 @@ __global__ void __launch_bounds__(WrCfg<D, M>::THREADS) window_ref_kernel(const 
         store4(out + c * 32 + tx * 4, x);
       }
       if (tx == 0 && prm.lse)
-        prm.lse[((size_t)b * prm.heads_q + h) * prm.n_q + row] = l[i] == 0.f ? -INFINITY : (m[i] + log2f(l[i])) * 0.6931471805599453f;
+        prm.lse[((size_t)b * prm.heads_q + h) * prm.n_q + row] = l[i] == 0.f ? -INFINITY : (m[i] + log2f(l[i] * kWeightBack)) * 0.6931471805599453f;
     }
   }
 }

@@ -137,6 +137,25 @@ def test_rows_that_are_not_numbers_where_they_are_seen():
     assert torch.isinf(O[1].float()).all() and torch.isnan(O[2].float()).all() and torch.isnan(lse[2]).all()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("n", [50, 3000])
+def test_the_largest_values_at_weights_of_zero(dtype, n):
+    """All keys but one are 400 octaves below it: their weights are zero in fp32, and their values, the largest of the type, nothing.  (Those
+    of a part of the rows without that key add up to more than fp32 holds.)"""
+    d = 64
+    cache = binding.PagedCache(binding.make_cache_problem(1, 2, 1, d, dtype, 16, 200, 200, softmax_scale=1.0), DEV,
+                               page_table=torch.arange(200, dtype=torch.int32, device=DEV)[None])
+    k, v = torch.zeros((2, 1, 1, n, d), dtype=DT[dtype], device=DEV)
+    k[..., 0], v[:] = -140.0, torch.finfo(DT[dtype]).max
+    at = n - 20
+    k[0, 0, at, 0], v[0, 0, at] = 140.0, torch.linspace(-1, 1, d, device=DEV).to(DT[dtype])
+    q = torch.zeros((1, 2, 1, d), dtype=DT[dtype], device=DEV)
+    q[..., 0] = 1.0
+    cache.cache_append(k, v)
+    O, lse = cache.paged_attention_fwd(q, appended=n)
+    check(cache, q, [n], O, lse)
+
+
 @pytest.mark.parametrize("spare", [0, 20])
 def test_bad_pages_and_lengths_are_recorded(spare):
     cache, q = make(5, [40, 40], 2, 1, 64, "bf16", 16, garbage=False, spare=spare)

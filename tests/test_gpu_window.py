@@ -182,6 +182,19 @@ def test_large_values_next_to_masked_ones():
         check(p, q, k, v, *run(p, q, k, v))
 
 
+@pytest.mark.parametrize("dtype,flags", KERNELS)
+@pytest.mark.parametrize("n", [40, 700])
+def test_sums_of_the_largest_values(dtype, flags, n):
+    """Values of half the largest number, whose sums overflow before the division; behind a key that takes all the weight, nothing."""
+    d, at = 64, n - 20
+    q, k, v = (torch.zeros((1, 1, n, d), dtype=DT[dtype], device=DEV) for _ in range(3))
+    q[..., 0], k[..., 0], v[:] = 1.0, -140.0, torch.finfo(DT[dtype]).max / 2
+    k[0, 0, at, 0], v[0, 0, at] = 140.0, torch.linspace(-1, 1, d, device=DEV).to(DT[dtype])
+    p = binding.make_window_problem(1, 1, 1, n, n, d, dtype, -1, 0, softmax_scale=1.0, flags=flags)
+    O, lse = run(p, q, k, v)
+    check(p, q, k, v, O, lse)
+
+
 def test_graphs_streams_and_shared_workspace():
     g = generator(4)
     plans = []
