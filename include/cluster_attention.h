@@ -308,7 +308,8 @@ typedef struct {
 /*
  * Q, K -> Qo, Ko with `n` rows at `positions` [batch, n, axes] int32 (device; batch items pos_stride_b
  * apart, 0: the same for all).  inverse != 0 turns by -t: the transpose, which carries gradients of the
- * rotated rows back.  heads_k may be 0 (K, Ko NULL).  An output may be its input, with the same strides.
+ * rotated rows back.  heads_k may be 0 (K, Ko NULL).  An output may be its input, with the same strides, and
+ * overlaps nothing else of the call.
  * No workspace.
  */
 int rotary_axes(const ca_rotary_t* rot, int32_t batch, int32_t heads_q, int32_t heads_k, int32_t n,
@@ -368,7 +369,8 @@ int paged_attention_fwd(const ca_cache_t* c, const ca_rows_t* Q, const void* K_p
  * query i at p = i + len_k - len_q.  It sees key j if
  *   j <= p + right   and   (j >= p - left   or   j < sinks);         a bound of -1 is none
  * (right = 0: causal; first tokens that stand behind p + right are not seen).  O = softmax-weighted mean of
- * the visible values, lse [batch, heads_q, n_q] fp32 or NULL; a row that sees nothing: zeros and -inf.  Rows from
+ * the visible values, lse [batch, heads_q, n_q] fp32 or NULL; a row that sees nothing: zeros and -inf.  O overlaps
+ * none of Q, K and V.  Rows from
  * len_q[b] on are left as they were, in O and lse, and rows of K and V from len_k[b] on are not used.
  * bf16 storage runs on tcgen05 tensor cores with fp32 accumulation and bf16 probabilities, fp32 storage on
  * products of tf32 halves with the accuracy of fp32; CA_ATTN_FP32 in flags selects the FP32 CUDA-core kernel,

@@ -587,6 +587,9 @@ int check_window(const ca_window_t* p) {
   if ((long long)p->batch * p->heads_q > 0x7fffffffLL) return CA_ERR_UNSUPPORTED;
   return CA_OK;
 }
+bool same_strides(const ca_rows_t* a, const ca_rows_t* b, int batch, int heads, int n) {
+  return (batch == 1 || a->stride_b == b->stride_b) && (heads == 1 || a->stride_h == b->stride_h) && (n == 1 || a->stride_n == b->stride_n);
+}
 float scale_of(float softmax_scale, int head_dim) { return softmax_scale > 0.f ? softmax_scale : 1.0f / sqrtf((float)head_dim); }
 }  // namespace
 
@@ -600,6 +603,12 @@ int rotary_axes(const ca_rotary_t* rot, int32_t batch, int32_t heads_q, int32_t 
   if (heads_k) {
     CA_TRY(check_rows(K, batch, heads_k, n, head_dim, dtype, false));
     CA_TRY(check_rows(Ko, batch, heads_k, n, head_dim, dtype, true));
+  }
+  // an output that is its input keeps the strides, and is no other tensor of the call
+  if (Q->data == Qo->data && !same_strides(Q, Qo, batch, heads_q, n)) return CA_ERR_INVALID_ARG;
+  if (heads_k) {
+    if (K->data == Ko->data && !same_strides(K, Ko, batch, heads_k, n)) return CA_ERR_INVALID_ARG;
+    if (Qo->data == Ko->data || Qo->data == K->data || Ko->data == Q->data) return CA_ERR_INVALID_ARG;
   }
   return launch_rotary_axes(*rot, batch, heads_q, heads_k, n, head_dim, dtype, inverse, Q, K, positions, pos_stride_b, Qo, Ko,
                             static_cast<cudaStream_t>(stream));
@@ -652,6 +661,8 @@ int window_attention_fwd(const ca_window_t* p, const ca_rows_t* Q, const ca_rows
   CA_TRY(check_rows(V, p->batch, p->heads_kv, p->n_k, p->head_dim, p->dtype, false));
   CA_TRY(check_rows(O, p->batch, p->heads_q, p->n_q, p->head_dim, p->dtype, true));
   if (!ws || !aligned16(ws) || ws_bytes < window_workspace_bytes(*p)) return CA_ERR_WORKSPACE;
+  // (rows that are computed again are read again when others have been written)
+  if (O->data == Q->data || O->data == K->data || O->data == V->data) return CA_ERR_INVALID_ARG;
   return launch_window(*p, Q, K, V, len_q, len_k, scale_of(p->softmax_scale, p->head_dim), O, lse, ws,
                        static_cast<cudaStream_t>(stream));
 }

@@ -43,6 +43,11 @@ def test_rotary_refusals(lib):
             assert call_rotary(lib, **{which: bad}) == INVALID, which
     for bad in (rows(n=0), rows(h=64), rows(b=-128)):       # rows of an output overlap
         assert call_rotary(lib, oq=bad) == INVALID and call_rotary(lib, ok=bad) == INVALID
+    # an output that is another tensor of the call, or its input with other strides
+    other = [rows(PTR + (i << 24)) for i in range(4)]
+    apart = dict(q=other[0], k=other[1], oq=other[2], ok=other[3])
+    for kw in (dict(oq=other[1]), dict(ok=other[0]), dict(ok=other[2]), dict(oq=rows(PTR, n=256)), dict(ok=rows(PTR + (1 << 24), b=1 << 17))):
+        assert call_rotary(lib, **{**apart, **kw}) == INVALID, kw
     good = (ctypes.c_double * 65)(*([1.0] * 65))
     ptr = ctypes.cast(good, ctypes.POINTER(ctypes.c_double))
     four = ctypes.c_int32 * 4
@@ -112,6 +117,9 @@ def test_window_refusals(lib):
     assert window(o=rows(n=32)) == INVALID
     for kw in (dict(ws=None), dict(ws=PTR + 4), dict(ws_bytes=255)):
         assert window(**kw) == WORKSPACE, kw
+    other = [rows(PTR + (i << 24)) for i in range(4)]
+    for i in range(3):                                      # the output is an input
+        assert window(*other[:3], o=other[i]) == INVALID
 
 
 def test_binding_refusals(lib):
