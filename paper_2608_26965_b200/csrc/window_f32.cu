@@ -1,6 +1,6 @@
 // Attention over a sliding window for fp32 storage, on m16n8k8 products of tf32 operands.
 //
-// tf32 has 11 significant bits, so each operand is split in two, x = hi + lo with hi = x rounded to tf32 and lo = the rest rounded
+// tf32 has 11 significant bits, so each operand is split in two, x = hi + lo with hi = x rounded to tf32 and lo = the rest cut
 // to tf32, and a product is lo hi + hi lo + hi hi: what is left out is 2^-22 of it.  The tensor core cuts its sums instead of rounding
 // them, which over long chains loses more than that (2.7e-6 of the result with one accumulator for all); so chains of upper parts are two
 // products long and are added up in fp32, and the small products have chains of their own: 3.2e-7 off where a plain fp32 form is
@@ -39,12 +39,14 @@ struct WfCfg {
 struct Split {
   uint32_t hi, lo;
 };
-// In integers and one subtraction (the conversion instruction runs at an eighth of their rate).  An infinity's hi is one and its lo no
-// number, and so is what comes of it.
+// In integers and one subtraction (the conversion instruction runs at an eighth of their rate).  The product looks at the upper 19 bits: of
+// lo, which has 12 significant ones at most, it cuts the last, 2^-24 of x.  (Rounding lo in integers too would carry the mantissa of a
+// number that is none, all ones, into its sign and make it zero, as it does for hi; so lo of what is no number, or infinite, is no
+// number, and so is what comes of it.)
 __device__ __forceinline__ Split split(float x) {
   Split s;
   s.hi = (__float_as_uint(x) + 0x1000u) & 0xffffe000u;
-  s.lo = __float_as_uint(x - __uint_as_float(s.hi)) + 0x1000u;       // (the product looks at the upper 19 bits)
+  s.lo = __float_as_uint(x - __uint_as_float(s.hi));
   return s;
 }
 __device__ __forceinline__ void mma1688(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {

@@ -138,6 +138,31 @@ def test_rows_that_are_not_numbers_where_they_are_seen():
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("spare", [0, 20])
+@pytest.mark.parametrize("kind", ["key", "infinite", "value"])
+def test_a_row_that_is_no_number_anywhere(dtype, spare, kind):
+    """One bad row in each sequence, at another place of a step and a unit in each."""
+    lengths = [130] * 130
+    cache, q = make(9, lengths, 2, 1, 64, dtype, 16, spare=spare)
+    q[..., 0] = q[..., 0].abs() + 0.5
+    items = torch.arange(130, device=DEV)
+    page = cache.page_table[items, items // 16].long()
+    words, nan = (torch.int16, 0x7fff) if dtype == "bf16" else (torch.int32, 0x7fffffff)
+    if kind == "key":
+        cache.K_pages.view(words)[page, 0, items % 16, 5] = nan
+    elif kind == "infinite":
+        cache.K_pages[page, 0, items % 16, 0] = math.inf
+    else:
+        cache.V_pages.view(words)[page, 0, items % 16, 3] = nan
+    O, lse = cache.paged_attention_fwd(q)
+    if kind == "value":
+        assert torch.isnan(O[..., 3]).all() and torch.isfinite(lse).all()
+        assert torch.isfinite(O.float()).sum() == O.numel() - O.numel() // 64
+    else:
+        assert torch.isnan(O).all() and torch.isnan(lse).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 @pytest.mark.parametrize("n", [50, 3000])
 def test_the_largest_values_at_weights_of_zero(dtype, n):
     """All keys but one are 400 octaves below it: their weights are zero in fp32, and their values, the largest of the type, nothing.  (Those
