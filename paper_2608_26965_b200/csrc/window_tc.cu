@@ -96,12 +96,18 @@ __device__ __forceinline__ f32x2 exp2_unit(f32x2 x) {
 }
 // 2^x without the special-function unit, for part of the scores (kWtEvery): x = j + f with j the nearest whole number, 2^f by a
 // polynomial of degree 5 (fitted to the smallest relative error on [-1/2, 1/2] with the constant term 1; 1.2e-7 with its roundings)
-// and j added to the exponent.  x at or below -127 gives exactly 0 (there the polynomial is 1, whose exponent field is 127), above 127 about 2^127,
-// which makes the sum leave the range as infinity would.
+// and j added to the exponent.  x at or below -127 gives exactly 0 (there the polynomial is 1, whose exponent field is 127), from 128 on exactly
+// infinity.  What is no number stays so up to the sum with the exponent, which makes the largest finite number of it (0x7fffffff +
+// (0x7fffffff << 23)): in bf16 that is infinity, so that O is not finite and the row is computed again.
+__device__ __forceinline__ float clamp_nan(float x) {
+  float y;
+  asm("{.reg .f32 t;\n\tmax.NaN.f32 t, %1, 0fC2FE0000;\n\tmin.NaN.f32 %0, t, 0f43000000;}" : "=f"(y) : "f"(x));       // -127, 128
+  return y;
+}
 __device__ __forceinline__ f32x2 exp2_fma(f32x2 x) {
   float a, b;
   unpack2(x, a, b);
-  x = pack2(fminf(fmaxf(a, -127.f), 127.f), fminf(fmaxf(b, -127.f), 127.f));
+  x = pack2(clamp_nan(a), clamp_nan(b));
   const f32x2 magic = pack2(12582912.f, 12582912.f), magic_neg = pack2(-12582912.f, -12582912.f);   // 1.5 2^23: j in the low bits
   const f32x2 shifted = add2(x, magic);
   const f32x2 f = fma2(add2(shifted, magic_neg), pack2(-1.f, -1.f), x);
@@ -584,13 +590,13 @@ window_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(b_p_ready(i));
-        if (big > kWtSumLimit) pend = ceilf(log2f(big));
+        if (big > kWtSumLimit) pend = fminf(ceilf(log2f(big)), 126.f);     // (2^-127 would be zero, and the sum so far lost)
         begun = true;
         ++steps;
       }
       if (!ok) break;
       // ---- O / l; a row that sees nothing: zeros, log-sum-exp -inf
-      const bool live = r < it.len_q, empty = l == 0.f;
+      const bool live = r < it.len_q, empty = l == 0.f && !(m > -INFINITY);
       const float inv = empty ? 0.f : 1.f / l;
       __nv_bfloat16* out = static_cast<__nv_bfloat16*>(prm.w.o) + w.b * prm.w.o_b + w.h * prm.w.o_h + r * prm.w.o_n;
       if (begun) {

@@ -183,6 +183,66 @@ def test_large_values_next_to_masked_ones():
 
 
 @pytest.mark.parametrize("dtype,flags", KERNELS)
+@pytest.mark.parametrize("second", [None, 0.0, -1.0, 3.0])
+def test_scores_that_jump_by_the_range_of_the_type(dtype, flags, second):
+    """A key some 2^120 to 2^130 times as heavy as those before it, and a second one `second` octaves from it, at any place of a step."""
+    jumps = [20.0, 31.0, 33.0, 60.0, 100.0, 119.0, 120.0, 124.0, 125.0, 125.5, 126.0, 126.5, 127.0, 127.5, 128.0, 129.0, 130.0, 150.0, 255.0, 1000.0]
+    B, n, d = 2 * len(jumps), 500, 64
+    g = generator(77)
+    q, k = (torch.zeros((B, 1, n, d), dtype=DT[dtype], device=DEV) for _ in range(2))
+    v = rows(g, (B, 1, n, d), dtype)
+    q[..., 0] = 1.0
+    for b in range(B):
+        x = jumps[b // 2]
+        k[b, 0, 130 + b, 0] = x                             # (even and odd places: exponentials of both units)
+        if second is not None:
+            k[b, 0, 290 + 3 * b, 0] = x + second
+    p = binding.make_window_problem(B, 1, 1, n, n, d, dtype, -1, 0, softmax_scale=math.log(2.0), flags=flags)
+    O, lse = run(p, q, k, v)
+    check(p, q, k, v, O, lse)
+
+
+@pytest.mark.parametrize("dtype,flags", KERNELS)
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("kind", ["key", "gpu's", "infinite", "value", "query"])
+@pytest.mark.parametrize("first", [0, 64])
+def test_numbers_that_are_none_inside_the_window(dtype, flags, d, kind, first):
+    """One bad row in each batch item, at 33 neighbouring places: the rows that see it are not numbers, the others as without it."""
+    B, n, left = 33, 200, 40
+    g = generator(d)
+    q, k, v = (rows(g, (B, 1, n, d), dtype) for _ in range(3))
+    q[..., 0] = q[..., 0].abs() + 0.5
+    p = binding.make_window_problem(B, 1, 1, n, n, d, dtype, left, 0, flags=flags)
+    bad = [x.clone() for x in (q, k, v)]
+    words = torch.int16 if dtype == "bf16" else torch.int32
+    nan = 0x7fff if dtype == "bf16" else 0x7fffffff
+    at, items = torch.arange(B, device=DEV) + first, torch.arange(B, device=DEV)
+    if kind == "key":
+        bad[1][items, 0, at] = math.nan
+    elif kind == "gpu's":
+        bad[1].view(words)[items, 0, at, 5] = nan
+    elif kind == "infinite":
+        bad[1][items, 0, at, 0] = math.inf
+    elif kind == "value":
+        bad[2].view(words)[items, 0, at, 3] = nan
+    else:
+        bad[0].view(words)[items, 0, at, 7] = nan
+    O, lse = run(p, *bad)
+    row = torch.arange(n, device=DEV)
+    hit = (row >= at[:, None]) & (row <= at[:, None] + (0 if kind == "query" else left))          # [B, n]
+    columns = torch.ones(d, dtype=torch.bool, device=DEV)
+    if kind == "value":
+        columns = torch.arange(d, device=DEV) == 3
+    wrong = hit[:, None, :, None] & columns
+    assert torch.isnan(O[wrong]).all(), int((~torch.isnan(O[wrong])).sum())
+    want, want_lse = run(p, q, k, v)
+    if kind != "value":
+        assert torch.isnan(lse[hit[:, None]]).all()
+        lse = torch.where(hit[:, None], want_lse, lse)
+    check(p, q, k, v, torch.where(wrong, want, O), lse)
+
+
+@pytest.mark.parametrize("dtype,flags", KERNELS)
 @pytest.mark.parametrize("n", [40, 700])
 def test_sums_of_the_largest_values(dtype, flags, n):
     """Values of half the largest number, whose sums overflow before the division; behind a key that takes all the weight, nothing."""
