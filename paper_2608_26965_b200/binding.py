@@ -409,8 +409,9 @@ class Plan:
         """Q and K turned by their positions (rotary_axes), in buffers of the plan."""
         p, dt = self.problem, torch_dtype(self.problem)
         if getattr(self, "Qr", None) is None:
-            self.Qr = torch.empty((p.batch, p.heads, p.n_q, p.head_dim), dtype=dt, device=self.device)
-            self.Kr = torch.empty((p.batch, p.heads, p.n_k, p.head_dim), dtype=dt, device=self.device)
+            with _SAME if stream is None else torch.cuda.stream(stream):         # in order with what the call's stream does
+                self.Qr = torch.empty((p.batch, p.heads, p.n_q, p.head_dim), dtype=dt, device=self.device)
+                self.Kr = torch.empty((p.batch, p.heads, p.n_k, p.head_dim), dtype=dt, device=self.device)
         if positions_k is None and p.n_q == p.n_k:
             return rotary_axes(rotary, Q, K, positions_q, out_q=self.Qr, out_k=self.Kr, stream=stream)
         rotary_axes(rotary, Q, None, positions_q, out_q=self.Qr, stream=stream)

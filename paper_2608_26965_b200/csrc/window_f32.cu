@@ -3,12 +3,12 @@
 // tf32 has 11 significant bits, so each operand is split in two, x = hi + lo with hi = x rounded to tf32 and lo = the rest cut
 // to tf32, and a product is lo hi + hi lo + hi hi: what is left out is 2^-22 of it.  The tensor core cuts its sums instead of rounding
 // them, which over long chains loses more than that (2.7e-6 of the result with one accumulator for all); so chains of upper parts are two
-// products long and are added up in fp32, and the small products have chains of their own: 3.2e-7 off where a plain fp32 form is
-// 6e-7 (12 heads of 1,370 rows, d = 64, 148 rows to either side).
+// products long and are added up in fp32, and the small products have chains of their own: 3.4e-7 off where a plain fp32 form is
+// 5.5e-7 (12 heads of 1,370 rows, d = 64, 148 rows to either side).
 //
 // Three products for one, at four times the rate of the CUDA cores' multiply-adds, and the operands come from shared memory a
 // word per lane and product: the 1,370 rows take 47 us (window_ref.cu, which waits for vectors of shared memory, 73), 2 x 8 heads of 4,000
-// rows, causal, d = 64, 500 rows before 233 us (331).  What bounds it is the chain of a warp's step (copy to registers, split,
+// rows, causal, d = 64, 500 rows before 229 us (331).  What bounds it is the chain of a warp's step (copy to registers, split,
 // product, softmax, product): tensor pipe 43 % busy, an instruction every third cycle, with the eight warps that 255 registers allow (168
 // registers and twelve warps: 55 us, 128 and sixteen: 76, for the registers that then go through memory).
 //
