@@ -595,8 +595,9 @@ window_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
         ++steps;
       }
       if (!ok) break;
-      // ---- O / l; a row that sees nothing: zeros, log-sum-exp -inf
-      const bool live = r < it.len_q, empty = l == 0.f && !(m > -INFINITY);
+      // ---- O / l; a row that sees nothing: zeros, log-sum-exp -inf.  (By the mask: m and l of a row whose scores are no numbers can be
+      // -inf and 0 too, since the sum so far is scaled by 0 while m is -inf; its O is not finite, and it is computed again.)
+      const bool live = r < it.len_q, empty = sees.end == 0;
       const float inv = empty ? 0.f : 1.f / l;
       __nv_bfloat16* out = static_cast<__nv_bfloat16*>(prm.w.o) + w.b * prm.w.o_b + w.h * prm.w.o_h + r * prm.w.o_n;
       if (begun) {
