@@ -2,6 +2,8 @@
 // is include/cluster_attention.h).  Every launcher enqueues on `st` and returns
 // a CA_* code.
 #pragma once
+#include <math.h>
+
 #include "common.cuh"
 
 namespace ca {
@@ -95,9 +97,19 @@ int launch_attn_ref(const ca_problem_t& pr, const void* Qp, const void* Kp, cons
                     float* lse, int* status, LaunchStream st, const int32_t* redo = nullptr, int redo_tiles = 0,
                     int* redo_count = nullptr);
 
-// Probabilities are summed 2^32 times smaller than they are: 2^31 of the largest finite values do not add up to infinity before the
-// division (an infinite sum that a new maximum then scales by zero would be a NaN).
-constexpr float kWeightScale = 0x1p-32f, kWeightBack = 0x1p32f;
+// Probabilities (exp2 gives the normal numbers from 2^-126 to 1) are taken 2^14 times larger than they are, so that the lower part of one that
+// is split in two is a normal number too, and what they make of small values loses no bits below the normal range.
+constexpr float kWeightScale = 0x1p14f, kWeightBack = 0x1p-14f;
+// Sums of values beyond 2^114 over the number of rows then pass fp32's range on the way to a mean that does not.  Means that come out as not
+// finite are taken again, from values 2^64 times smaller, with weights in one piece.
+constexpr float kValueScale = 0x1p-64f, kValueBack = 0x1p64f;
+// the mean of a column from its sum of small values: of finite values it is none beyond the type's largest, whatever the roundings
+template <typename T>
+__device__ __forceinline__ float mean_of_small(float sum, float l) {
+  constexpr float most = sizeof(T) == 2 ? 0x1.fep127f : 0x1.fffffep127f;
+  const float x = sum / l;
+  return fabsf(x) < INFINITY ? fminf(fmaxf(x * kValueBack, -most), most) : x;
+}
 
 // rotary.cu
 int check_rows(const ca_rows_t* x, int batch, int heads, int n, int D, int dtype, bool written);

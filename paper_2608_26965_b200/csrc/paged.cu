@@ -175,6 +175,7 @@ template <int D, int NT>
 struct WarpMma {
   using T = __nv_bfloat16;
   static constexpr int ROWS = 8 * NT, KEYS = 16, STAGES = NT == 1 ? 3 : 2;
+  static constexpr int CTAS = 5 - NT - D / 128;   // to an SM, by registers: 128, 168 or 255
   static constexpr int ROW_BYTES = D * 2, CHUNKS = ROW_BYTES / 16;
   uint32_t q[NT][D / 16][2], coming[NT][D / 16][2];
   float o[NT][D / 16][4];
@@ -253,9 +254,9 @@ struct WarpMma {
 #pragma unroll
           for (int i = 0; i < 4; ++i) o[t][n][i] *= by[i & 1];
       }
-      // Probabilities in two bf16 parts, the upper bits and the rest: the products have time to spare, and the result the accuracy of
-      // fp32.  The rest is at least 2^-24 of the probability, half a step of fp32: where it is zero, 0 x infinity would make an infinite
-      // value a NaN, and of a weight that is itself zero it stays zero, however large the value.
+      // Probabilities in two bf16 parts, the upper bits and the rest, since the products have time to spare: a weight is off by 2^-16 of
+      // itself (the rest is below 2^-8 of it and rounded by 2^-8).  The rest is at least 2^-24 of the probability: where it is zero, 0 x
+      // infinity would make an infinite value a NaN, and of a weight that is itself zero it stays zero, however large the value.
       const float ref0 = m[t][0] == -INFINITY ? 0.f : -m[t][0], ref1 = m[t][1] == -INFINITY ? 0.f : -m[t][1];
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
@@ -308,6 +309,7 @@ template <int D, int R>
 struct WarpFma {
   using T = float;
   static constexpr int ROWS = R, KEYS = 8, STAGES = 3;
+  static constexpr int CTAS = D == 128 ? (R > 2 ? 1 : 2) : R > 1 ? 3 : 4;   // to an SM, by shared memory and by registers
   static constexpr int ROW_BYTES = D * 4, CHUNKS = ROW_BYTES / 16;
   static constexpr int SPLIT = 128 / D;      // keys that are worked on side by side in P V
   static constexpr bool HELD = R * D <= 256; // query rows in registers (a quarter of each: R D / 4), otherwise in shared memory
@@ -506,17 +508,96 @@ struct Place {
   }
 };
 
-// four columns of the result; a row that sees nothing: zero, log-sum-exp -inf
+// four columns of the mean; of a row that sees nothing zeros
+__device__ __forceinline__ float4 mean_of(float4 o, float l) {
+  return l == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(o.x / l, o.y / l, o.z / l, o.w / l);
+}
+// whether they are to be taken again: not finite, though the weights are
+__device__ __forceinline__ bool beyond(float4 mean, float l) {
+  return l < INFINITY && !(fabsf(mean.x) < INFINITY && fabsf(mean.y) < INFINITY && fabsf(mean.z) < INFINITY && fabsf(mean.w) < INFINITY);
+}
 template <typename T>
-__device__ __forceinline__ void finish_row(const PagedParams& prm, int b, int head, int col, float4 o, float m, float l) {
-  if (l == 0.f) o = make_float4(0.f, 0.f, 0.f, 0.f);
-  else o = make_float4(o.x / l, o.y / l, o.z / l, o.w / l);
-  store4(static_cast<T*>(prm.o) + b * prm.o_b + head * prm.o_h + col, o);
+__device__ __forceinline__ float4 replaced(float4 mean, float4 small, float l) {
+  if (!(fabsf(mean.x) < INFINITY)) mean.x = mean_of_small<T>(small.x, l);
+  if (!(fabsf(mean.y) < INFINITY)) mean.y = mean_of_small<T>(small.y, l);
+  if (!(fabsf(mean.z) < INFINITY)) mean.z = mean_of_small<T>(small.z, l);
+  if (!(fabsf(mean.w) < INFINITY)) mean.w = mean_of_small<T>(small.w, l);
+  return mean;
+}
+// Sums of weighted small values of a query head, by a warp: of the visible rows, 32 at a time, groups first, first + step, ... .  A lane
+// weighs one of the 32, then has columns lane D / 32 and the next.  Slow (some 150 cycles a row and warp), and hardly ever called.
+template <typename T, int D>
+__device__ __noinline__ float4 small_sums(const PagedParams& prm, int b, int h, int head, float m, int first, int step) {
+  const int lane = threadIdx.x & 31;
+  const Span span(prm, b, 32);
+  const int count = span.sink_end + span.n - span.lo;
+  const T* q = static_cast<const T*>(prm.q) + b * prm.q_b + head * prm.q_h;
+  float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 1
+  for (int c = first * 32; c < count; c += step * 32) {
+    float weight = 0.f;
+    long long at = -1;                         // (a row of a page that is none is zero, key and value)
+    if (c + lane < count) {
+      const int j = c + lane < span.sink_end ? c + lane : span.lo + (c + lane - span.sink_end);
+      const int page = prm.page_table[(size_t)b * prm.pages_per_sequence + j / prm.page_rows];
+      float s = 0.f;
+      if ((unsigned)page < (unsigned)prm.pages) {
+        at = (((long long)page * prm.heads_kv + h) * prm.page_rows + j % prm.page_rows) * D;
+        const T* k = static_cast<const T*>(prm.k_pages) + at;
+#pragma unroll 4
+        for (int i = 0; i < D; i += 4) {
+          const float4 x = load4(q + i), y = load4(k + i);
+          s = fmaf(x.x, y.x, fmaf(x.y, y.y, fmaf(x.z, y.z, fmaf(x.w, y.w, s))));
+        }
+      }
+      weight = ex2_approx(fmaf(s, prm.scale_log2, -m)) * kWeightScale;
+    }
+    const int rows = min(32, count - c);
+#pragma unroll 4
+    for (int i = 0; i < rows; ++i) {
+      const float w = __shfl_sync(0xffffffffu, weight, i);
+      const long long from = __shfl_sync(0xffffffffu, at, i);
+      if (from < 0) continue;
+      const T* v = static_cast<const T*>(prm.v_pages) + from + lane * (D / 32);
+      sum.x = fmaf(w, to_f32<T>(v[0]) * kValueScale, sum.x);
+      sum.y = fmaf(w, to_f32<T>(v[1]) * kValueScale, sum.y);
+      if (D == 128) {
+        sum.z = fmaf(w, to_f32<T>(v[2 % (D / 32)]) * kValueScale, sum.z);
+        sum.w = fmaf(w, to_f32<T>(v[3 % (D / 32)]) * kValueScale, sum.w);
+      }
+    }
+  }
+  return sum;
+}
+// The means of a warp, four columns to a lane (at d = 64 of two query heads), where some are to be taken again.
+template <typename T, int D>
+__device__ __noinline__ float4 taken_again(const PagedParams& prm, int b, int h, int head, float4 mean, float m, float l) {
+  constexpr int LANES = D / 4;
+  const int lane = threadIdx.x & 31;
+  const bool need = beyond(mean, l);
+#pragma unroll 1
+  for (int side = 0; side < 32 / LANES; ++side) {
+    const bool mine = lane / LANES == side;
+    if (!__any_sync(0xffffffffu, need && mine)) continue;
+    float4 s = small_sums<T, D>(prm, b, h, __shfl_sync(0xffffffffu, head, side * LANES), __shfl_sync(0xffffffffu, m, side * LANES), 0, 1);
+    if (D == 64) {                             // two lanes' columns are the four of one
+      const int a = lane % LANES * 2;
+      s = make_float4(__shfl_sync(0xffffffffu, s.x, a), __shfl_sync(0xffffffffu, s.y, a), __shfl_sync(0xffffffffu, s.x, a + 1), __shfl_sync(0xffffffffu, s.y, a + 1));
+    }
+    if (mine) mean = replaced<T>(mean, s, l);
+  }
+  return mean;
+}
+
+// four columns of the result; a row that sees nothing has a log-sum-exp of -inf
+template <typename T>
+__device__ __forceinline__ void finish_row(const PagedParams& prm, int b, int head, int col, float4 mean, float m, float l) {
+  store4(static_cast<T*>(prm.o) + b * prm.o_b + head * prm.o_h + col, mean);
   if (col == 0 && prm.lse) prm.lse[(size_t)b * prm.heads_q + head] = l == 0.f ? -INFINITY : (m + log2f(l * kWeightBack)) * 0.6931471805599453f;
 }
 
 template <typename W, int D>
-__global__ void __launch_bounds__(kPagedThreads) paged_kernel(const __grid_constant__ PagedParams prm) {
+__global__ void __launch_bounds__(kPagedThreads, W::CTAS) paged_kernel(const __grid_constant__ PagedParams prm) {
   using C = PagedCfg<W, D>;
   using T = typename W::T;
   extern __shared__ __align__(128) unsigned char smem[];
@@ -683,8 +764,9 @@ __global__ void __launch_bounds__(kPagedThreads) paged_kernel(const __grid_const
     w.put(mine, ml + warp * 2 * W::ROWS, rows, lane);
     __syncthreads();
     float* part = prm.partial + (size_t)(2 * blockIdx.x + (first_tile == 0 ? 1 : 0)) * W::ROWS * (D + 4);
-    for (int i = threadIdx.x; i < rows * (D / 4); i += kPagedThreads) {
-      const int r = i / (D / 4), col = i % (D / 4) * 4;
+    for (int first = warp * 32; first < rows * (D / 4); first += kPagedThreads) {      // (by whole warps)
+      const int i = first + lane, r = min(i / (D / 4), rows - 1), col = i % (D / 4) * 4;
+      const bool live = i < rows * (D / 4);
       float top = -INFINITY, l = 0.f;
       float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
@@ -697,8 +779,10 @@ __global__ void __launch_bounds__(kPagedThreads) paged_kernel(const __grid_const
         l = fmaf(ml[(x * W::ROWS + r) * 2 + 1], by, l);
       }
       if (whole) {
-        finish_row<T>(prm, at.b, head0 + r, col, o, top, l);
-      } else {
+        float4 mean = mean_of(o, l);
+        if (__any_sync(0xffffffffu, beyond(mean, l))) mean = taken_again<T, D>(prm, at.b, at.h, head0 + r, mean, top, l);
+        if (live) finish_row<T>(prm, at.b, head0 + r, col, mean, top, l);
+      } else if (live) {
         *reinterpret_cast<float4*>(part + r * D + col) = o;
         if (col == 0) *reinterpret_cast<float2*>(part + W::ROWS * D + 2 * r) = make_float2(top, l);
       }
@@ -733,7 +817,7 @@ __global__ void __launch_bounds__(kPagedThreads) paged_kernel(const __grid_const
 // have the loads of eight parts in flight; then the groups are joined in shared memory.
 constexpr int kJoinThreads = 256, kJoinRows = 2;
 template <typename W, int D>
-__global__ void __launch_bounds__(kJoinThreads) paged_join_kernel(const __grid_constant__ PagedParams prm, int ctas) {
+__global__ void __launch_bounds__(kJoinThreads, 3) paged_join_kernel(const __grid_constant__ PagedParams prm, int ctas) {
   using C = PagedCfg<W, D>;
   wait_for_previous();
   let_next_start();
@@ -794,19 +878,49 @@ __global__ void __launch_bounds__(kJoinThreads) paged_join_kernel(const __grid_c
   sum[g][item] = o;
   ml[g][item] = make_float2(top, l);
   __syncthreads();
-  if (g > 0 || item / (D / 4) >= rows) return;
+  const int head0 = h * prm.group + rt * W::ROWS + row0;
+  float4 mean = make_float4(0.f, 0.f, 0.f, 0.f);
+  if (g == 0) {
 #pragma unroll
-  for (int k = 1; k < GROUPS; ++k) top = fmaxf(top, ml[k][item].x);
-  const float own = ml[0][item].x == -INFINITY ? 0.f : ex2_approx(ml[0][item].x - top);
-  o.x *= own; o.y *= own; o.z *= own; o.w *= own;
-  l *= own;
+    for (int k = 1; k < GROUPS; ++k) top = fmaxf(top, ml[k][item].x);
+    const float own = ml[0][item].x == -INFINITY ? 0.f : ex2_approx(ml[0][item].x - top);
+    o.x *= own; o.y *= own; o.z *= own; o.w *= own;
+    l *= own;
 #pragma unroll
-  for (int k = 1; k < GROUPS; ++k) {
-    const float wk = ml[k][item].x == -INFINITY ? 0.f : ex2_approx(ml[k][item].x - top);
-    add_scaled(o, sum[k][item], wk);
-    l = fmaf(ml[k][item].y, wk, l);
+    for (int k = 1; k < GROUPS; ++k) {
+      const float wk = ml[k][item].x == -INFINITY ? 0.f : ex2_approx(ml[k][item].x - top);
+      add_scaled(o, sum[k][item], wk);
+      l = fmaf(ml[k][item].y, wk, l);
+    }
+    mean = mean_of(o, l);
+    ml[0][item].x = top;
   }
-  finish_row<typename W::T>(prm, b, h * prm.group + rt * W::ROWS + row0 + r, col, o, top, l);
+  if (__syncthreads_or(g == 0 && beyond(mean, l))) {
+    // again, by all warps; their sums by way of `sum`
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    float* all = reinterpret_cast<float*>(sum);
+    static_assert(kJoinThreads / 32 * D <= GROUPS * ITEMS * 4, "a row of each warp");
+#pragma unroll 1
+    for (int x = 0; x < rows; ++x) {
+      const float4 s = small_sums<typename W::T, D>(prm, b, h, head0 + x, ml[0][x * (D / 4)].x, warp, kJoinThreads / 32);
+      float* to = all + warp * D + lane * (D / 32);
+      to[0] = s.x;
+      to[1] = s.y;
+      if (D == 128) { to[2 % (D / 32)] = s.z; to[3 % (D / 32)] = s.w; }
+      __syncthreads();
+      if (g == 0 && item / (D / 4) == x && beyond(mean, l)) {
+        float4 t = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int w = 0; w < kJoinThreads / 32; ++w) {
+          const float4 y = *reinterpret_cast<const float4*>(all + w * D + col);
+          t = make_float4(t.x + y.x, t.y + y.y, t.z + y.z, t.w + y.w);
+        }
+        mean = replaced<typename W::T>(mean, t, l);
+      }
+      __syncthreads();
+    }
+  }
+  if (g == 0 && item / (D / 4) < rows) finish_row<typename W::T>(prm, b, head0 + r, col, mean, top, l);
 }
 
 // ---- host side -------------------------------------------------------------------------------------------

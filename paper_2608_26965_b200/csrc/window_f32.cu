@@ -17,7 +17,8 @@
 //     S = Q K^T      a thread holds rows lane/4 and lane/4 + 8, keys 2 (lane % 4) and the next of every 8
 //     O += P V       P as it is held: its keys 2 t and 2 t + 1 stand at columns t and t + 4 of the product, and V's rows likewise
 // Masked probabilities are 0, and 0 x infinity is not: rows whose result is not finite are marked and computed again by the
-// CUDA-core kernel (as those of the bf16 kernel are).
+// CUDA-core kernel (as those of the bf16 kernel are).  So are rows with a result below 2^-100 that is not zero: of a value below some 2^-112
+// the lower half is below the normal range, where tf32 has only ten bits behind 2^-126.
 #include <math.h>
 
 #include "tc_ptx.cuh"
@@ -181,7 +182,7 @@ __global__ void __launch_bounds__(kWfThreads) window_f32_kernel(const __grid_con
     for (int n = 0; n < kWfKeys / 8; ++n)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const float p = ex2_approx(fmaf(s[n][i], prm.scale_log2, i < 2 ? ref0 : ref1));
+        const float p = ex2_approx(fmaf(s[n][i], prm.scale_log2, i < 2 ? ref0 : ref1)) * kWeightScale;
         l[i >> 1] += p;
         const Split x = split(p);
         const int at = (i >> 1) + (i & 1) * 2;          // (row, key) of the score -> place of the operand
@@ -216,12 +217,12 @@ __global__ void __launch_bounds__(kWfThreads) window_f32_kernel(const __grid_con
 #pragma unroll
     for (int n = 0; n < D / 8; ++n) {
       const float x = empty ? 0.f : o[n][2 * r] / l[r], y = empty ? 0.f : o[n][2 * r + 1] / l[r];
-      any += fabsf(x) + fabsf(y);
+      any += (x != 0.f && fabsf(x) < 0x1p-100f) || (y != 0.f && fabsf(y) < 0x1p-100f) ? INFINITY : fabsf(x) + fabsf(y);
       *reinterpret_cast<float2*>(out + n * 8) = make_float2(x, y);
     }
     any += empty ? 0.f : l[r];
     if (t4 == 0 && prm.lse)
-      prm.lse[((size_t)b * prm.heads_q + h) * prm.n_q + row] = empty ? -INFINITY : (m[r] + log2f(l[r])) * 0.6931471805599453f;
+      prm.lse[((size_t)b * prm.heads_q + h) * prm.n_q + row] = empty ? -INFINITY : (m[r] + log2f(l[r] * kWeightBack)) * 0.6931471805599453f;
   }
   const bool again = __any_sync(0xffffffffu, !(any < INFINITY));
   if (lane == 0) {

@@ -9,7 +9,7 @@
 // registers and warps).  M = 64 with R = 4; M = 32 with R = 2 where tiles of 64 rows would be fewer than one to an SM (100 rows, one
 // head: 10.4 us instead of 15.4).
 // Only tiles at a border of the window are masked: what a row does not see takes no part, whatever stands there
-// (0 x infinity would).
+// (0 x infinity would).  Rows with a mean that is not finite are gone over a second time, with small values (kernels.h).
 #include <math.h>
 
 #include <type_traits>
@@ -111,119 +111,138 @@ __global__ void __launch_bounds__(WrCfg<D, M>::THREADS) window_ref_kernel(const 
     };
     __syncthreads();                            // the rows before have been worked off
     window_rows_to_smem<T, D, C::THREADS, M>(sq, q, prm.q_n, rows, tid);
-    if (span.tiles > 0) fetch(0);
 
-    f32x2 o[R][D / 32][2];
-    float m[R], l[R];
-#pragma unroll
-    for (int i = 0; i < R; ++i) {
-      m[i] = -INFINITY;
-      l[i] = 0.f;
-#pragma unroll
-      for (int c = 0; c < D / 32; ++c) o[i][c][0] = o[i][c][1] = pack2(0.f, 0.f);
-    }
+    unsigned again[R] = {};                     // bits of this thread's columns that are to be taken again
 #pragma unroll 1
-    for (int t = 0; t < span.tiles; ++t) {
-      const int j0 = span.tile(t) * kWrKeys;
-      arrived();                                // and the tile before has been read
-      if (t + 1 < span.tiles) fetch(t + 1);
-      const float* sk = smf + C::OFF_KV + (t & 1) * 2 * C::KV;
-      const float* sv = sk + C::KV;
-      // ---- scores of rows R ty .. R ty + R - 1, keys tx, tx + 8, ...
-      f32x2 s2[R][4];
+    for (int pass = 0; pass < 2; ++pass) {
+      if (span.tiles > 0) fetch(0);
+      f32x2 o[R][D / 32][2];
+      float m[R], l[R];
 #pragma unroll
-      for (int i = 0; i < R; ++i)
+      for (int i = 0; i < R; ++i) {
+        m[i] = -INFINITY;
+        l[i] = 0.f;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) s2[i][j] = pack2(0.f, 0.f);
-#pragma unroll 4
-      for (int c = 0; c < D; c += 4) {
-        float4 a[R], x[4];
-#pragma unroll
-        for (int i = 0; i < R; ++i) a[i] = *reinterpret_cast<const float4*>(sq + (R * ty + i) * C::PITCH + c);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) x[j] = *reinterpret_cast<const float4*>(sk + (tx + 8 * j) * C::PITCH + c);
+        for (int c = 0; c < D / 32; ++c) o[i][c][0] = o[i][c][1] = pack2(0.f, 0.f);
+      }
+#pragma unroll 1
+      for (int t = 0; t < span.tiles; ++t) {
+        const int j0 = span.tile(t) * kWrKeys;
+        arrived();                                // and the tile before has been read
+        if (t + 1 < span.tiles) fetch(t + 1);
+        const float* sk = smf + C::OFF_KV + (t & 1) * 2 * C::KV;
+        const float* sv = sk + C::KV;
+        // ---- scores of rows R ty .. R ty + R - 1, keys tx, tx + 8, ...
+        f32x2 s2[R][4];
 #pragma unroll
         for (int i = 0; i < R; ++i)
 #pragma unroll
-          for (int j = 0; j < 4; ++j)
-            s2[i][j] = fma2(pack2(a[i].z, a[i].w), pack2(x[j].z, x[j].w), fma2(pack2(a[i].x, a[i].y), pack2(x[j].x, x[j].y), s2[i][j]));
+          for (int j = 0; j < 4; ++j) s2[i][j] = pack2(0.f, 0.f);
+#pragma unroll 4
+        for (int c = 0; c < D; c += 4) {
+          float4 a[R], x[4];
+#pragma unroll
+          for (int i = 0; i < R; ++i) a[i] = *reinterpret_cast<const float4*>(sq + (R * ty + i) * C::PITCH + c);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) x[j] = *reinterpret_cast<const float4*>(sk + (tx + 8 * j) * C::PITCH + c);
+#pragma unroll
+          for (int i = 0; i < R; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+              s2[i][j] = fma2(pack2(a[i].z, a[i].w), pack2(x[j].z, x[j].w), fma2(pack2(a[i].x, a[i].y), pack2(x[j].x, x[j].y), s2[i][j]));
+        }
+        const bool whole = span.whole(j0, j0 + kWrKeys);
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+          const WindowRow row(prm, it, r0 + R * ty + i);
+          bool seen[4];
+          float s[4], top = m[i];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            float even, odd;
+            unpack2(s2[i][j], even, odd);
+            seen[j] = whole || row.sees(j0 + tx + 8 * j);
+            s[j] = seen[j] ? (even + odd) * prm.scale_log2 : -INFINITY;
+            top = fmaxf(top, s[j]);
+          }
+#pragma unroll
+          for (int x = 1; x < 8; x <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
+          const float by = m[i] == -INFINITY ? 0.f : ex2_approx(m[i] - top), ref = top == -INFINITY ? 0.f : top;
+          m[i] = top;
+          l[i] *= by;
+#pragma unroll
+          for (int c = 0; c < D / 32; ++c) {
+            o[i][c][0] = mul2(o[i][c][0], pack2(by, by));
+            o[i][c][1] = mul2(o[i][c][1], pack2(by, by));
+          }
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const float p = ex2_approx(s[j] - ref) * kWeightScale;
+            if (seen[j]) l[i] += p;
+            sp[(R * ty + i) * C::P_PITCH + tx + 8 * j] = seen[j] ? p : -1.f;      // (no probability: takes no part)
+          }
+        }
+        __syncwarp();                             // the rows of a warp's probabilities are its own
+        auto values = [&](auto masked, auto small) {
+#pragma unroll 2
+          for (int j = 0; j < kWrKeys; j += 4) {
+            float p[R][4];
+#pragma unroll
+            for (int i = 0; i < R; ++i) *reinterpret_cast<float4*>(p[i]) = *reinterpret_cast<const float4*>(sp + (R * ty + i) * C::P_PITCH + j);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+#pragma unroll
+              for (int c = 0; c < D / 32; ++c) {
+                float4 x = *reinterpret_cast<const float4*>(sv + (j + e) * C::PITCH + c * 32 + tx * 4);
+                if (decltype(small)::value) x = make_float4(x.x * kValueScale, x.y * kValueScale, x.z * kValueScale, x.w * kValueScale);
+#pragma unroll
+                for (int i = 0; i < R; ++i) {
+                  if (decltype(masked)::value && p[i][e] == -1.f) continue;
+                  o[i][c][0] = fma2(pack2(p[i][e], p[i][e]), pack2(x.x, x.y), o[i][c][0]);
+                  o[i][c][1] = fma2(pack2(p[i][e], p[i][e]), pack2(x.z, x.w), o[i][c][1]);
+                }
+              }
+          }
+        };
+        if (pass == 1) values(std::true_type{}, std::true_type{});
+        else if (whole) values(std::false_type{}, std::false_type{});
+        else values(std::true_type{}, std::false_type{});
       }
-      const bool whole = span.whole(j0, j0 + kWrKeys);
+      if (std::is_same<T, float>::value) asm volatile("cp.async.wait_all;" ::: "memory");
+      bool any = false;
 #pragma unroll
       for (int i = 0; i < R; ++i) {
-        const WindowRow row(prm, it, r0 + R * ty + i);
-        bool seen[4];
-        float s[4], top = m[i];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          float even, odd;
-          unpack2(s2[i][j], even, odd);
-          seen[j] = whole || row.sees(j0 + tx + 8 * j);
-          s[j] = seen[j] ? (even + odd) * prm.scale_log2 : -INFINITY;
-          top = fmaxf(top, s[j]);
-        }
-#pragma unroll
-        for (int x = 1; x < 8; x <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
-        const float by = m[i] == -INFINITY ? 0.f : ex2_approx(m[i] - top), ref = top == -INFINITY ? 0.f : top;
-        m[i] = top;
-        l[i] *= by;
+        for (int x = 1; x < 8; x <<= 1) l[i] += __shfl_xor_sync(0xffffffffu, l[i], x);
+        const int row = r0 + R * ty + i;
+        if (row >= it.len_q) continue;
+        // a row that sees nothing: zeros, log-sum-exp -inf
+        T* out = static_cast<T*>(prm.o) + b * prm.o_b + h * prm.o_h + row * prm.o_n;
 #pragma unroll
         for (int c = 0; c < D / 32; ++c) {
-          o[i][c][0] = mul2(o[i][c][0], pack2(by, by));
-          o[i][c][1] = mul2(o[i][c][1], pack2(by, by));
-        }
+          float x[4] = {0.f, 0.f, 0.f, 0.f};
+          if (l[i] != 0.f) {
+            unpack2(o[i][c][0], x[0], x[1]);
+            unpack2(o[i][c][1], x[2], x[3]);
+          }
+          if (pass == 1) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const float p = ex2_approx(s[j] - ref) * kWeightScale;
-          if (seen[j]) l[i] += p;
-          sp[(R * ty + i) * C::P_PITCH + tx + 8 * j] = seen[j] ? p : -1.f;      // (no probability: takes no part)
+            for (int e = 0; e < 4; ++e)
+              if (again[i] >> (4 * c + e) & 1u) out[c * 32 + tx * 4 + e] = from_f32<T>(mean_of_small<T>(x[e], l[i]));
+            continue;
+          }
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            if (l[i] != 0.f) x[e] = x[e] / l[i];
+            if (l[i] < INFINITY && !(fabsf(x[e]) < INFINITY)) again[i] |= 1u << (4 * c + e);
+          }
+          store4(out + c * 32 + tx * 4, make_float4(x[0], x[1], x[2], x[3]));
         }
+        any = any || again[i] != 0;
+        if (tx == 0 && prm.lse && pass == 0)
+          prm.lse[((size_t)b * prm.heads_q + h) * prm.n_q + row] = l[i] == 0.f ? -INFINITY : (m[i] + log2f(l[i] * kWeightBack)) * 0.6931471805599453f;
       }
-      __syncwarp();                             // the rows of a warp's probabilities are its own
-      auto values = [&](auto masked) {
-#pragma unroll 2
-        for (int j = 0; j < kWrKeys; j += 4) {
-          float p[R][4];
-#pragma unroll
-          for (int i = 0; i < R; ++i) *reinterpret_cast<float4*>(p[i]) = *reinterpret_cast<const float4*>(sp + (R * ty + i) * C::P_PITCH + j);
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-#pragma unroll
-            for (int c = 0; c < D / 32; ++c) {
-              const float4 x = *reinterpret_cast<const float4*>(sv + (j + e) * C::PITCH + c * 32 + tx * 4);
-#pragma unroll
-              for (int i = 0; i < R; ++i) {
-                if (decltype(masked)::value && p[i][e] == -1.f) continue;
-                o[i][c][0] = fma2(pack2(p[i][e], p[i][e]), pack2(x.x, x.y), o[i][c][0]);
-                o[i][c][1] = fma2(pack2(p[i][e], p[i][e]), pack2(x.z, x.w), o[i][c][1]);
-              }
-            }
-        }
-      };
-      if (whole) values(std::false_type{});
-      else values(std::true_type{});
-    }
-    if (std::is_same<T, float>::value) asm volatile("cp.async.wait_all;" ::: "memory");
-#pragma unroll
-    for (int i = 0; i < R; ++i) {
-#pragma unroll
-      for (int x = 1; x < 8; x <<= 1) l[i] += __shfl_xor_sync(0xffffffffu, l[i], x);
-      const int row = r0 + R * ty + i;
-      if (row >= it.len_q) continue;
-      // a row that sees nothing: zeros, log-sum-exp -inf
-      T* out = static_cast<T*>(prm.o) + b * prm.o_b + h * prm.o_h + row * prm.o_n;
-#pragma unroll
-      for (int c = 0; c < D / 32; ++c) {
-        float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (l[i] != 0.f) {
-          unpack2(o[i][c][0], x.x, x.y);
-          unpack2(o[i][c][1], x.z, x.w);
-          x = make_float4(x.x / l[i], x.y / l[i], x.z / l[i], x.w / l[i]);
-        }
-        store4(out + c * 32 + tx * 4, x);
-      }
-      if (tx == 0 && prm.lse)
-        prm.lse[((size_t)b * prm.heads_q + h) * prm.n_q + row] = l[i] == 0.f ? -INFINITY : (m[i] + log2f(l[i] * kWeightBack)) * 0.6931471805599453f;
+      if (pass == 0 && !__syncthreads_or(any)) break;      // (a barrier before the keys are fetched again, too)
     }
   }
 }

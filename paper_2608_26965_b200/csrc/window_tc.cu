@@ -618,7 +618,7 @@ window_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
           const f32x2 y = mul2(pack2(__uint_as_float(o[2 * e]), __uint_as_float(o[2 * e + 1])), pack2(inv, inv));
-          any2 = add2(any2, y);
+          any2 = fma2(y, pack2(1.01f, 1.01f), any2);       // (what rounds beyond bf16's largest number counts as not finite)
           float y0, y1;
           unpack2(y, y0, y1);
           x[e] = empty ? 0u : pack_bf16x2(y0, y1);
