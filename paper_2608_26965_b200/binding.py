@@ -193,6 +193,24 @@ def _require_cuda(t: torch.Tensor, name: str) -> None:
         raise ClusterAttnError(f"{name} must be contiguous")
 
 
+_SAME = contextlib.nullcontext()
+
+
+def _on(stream: Optional[torch.cuda.Stream]):
+    """Where a call makes buffers: in order with what its stream does."""
+    return _SAME if stream is None else torch.cuda.stream(stream)
+
+
+def _filled(device: torch.device) -> None:
+    """Waits for the fills of buffers that were just made: the calls take any stream, and nothing orders it behind the one that
+    the buffers were made on.  (In a capture nothing runs yet, and the fills are part of it.)"""
+    stream = torch.cuda.current_stream(device)
+    with torch.cuda.device(device):
+        capturing = torch.cuda.is_current_stream_capturing()
+    if not capturing:
+        stream.synchronize()
+
+
 def _ptr(t: Optional[torch.Tensor]):
     return None if t is None else ctypes.c_void_p(t.data_ptr())
 
@@ -279,6 +297,7 @@ class Plan:
         self.Yk = torch.empty((B, H, p.n_k, D), dtype=f32, device=dev) if keep_y else None
         sizes = workspace_bytes(p)
         self.ws = {k: torch.zeros(max(v, 256), dtype=torch.uint8, device=dev) for k, v in sizes.items()}
+        _filled(dev)
 
     # -- the three entry points ------------------------------------------------
     def cluster_qk(self, Q, K, V, Yq=None, Yk=None, stream=None):
@@ -352,10 +371,11 @@ class Plan:
         if p.flags & CA_METRIC_IN and (A_q is None or A_k is None):
             raise ClusterAttnError("CA_METRIC_IN needs A_q and A_k")
         shape = (p.batch, p.heads, p.head_dim, p.head_dim)
-        self.A_q = A_q if A_q is not None else torch.empty(shape, dtype=torch.float32, device=self.device)
-        self.A_k = A_k if A_k is not None else torch.empty(shape, dtype=torch.float32, device=self.device)
-        if self.ws.get("basic") is None or self.ws["basic"].numel() < nbytes:
-            self.ws["basic"] = torch.zeros(max(nbytes, 256), dtype=torch.uint8, device=self.device)
+        with _on(stream):
+            self.A_q = A_q if A_q is not None else torch.empty(shape, dtype=torch.float32, device=self.device)
+            self.A_k = A_k if A_k is not None else torch.empty(shape, dtype=torch.float32, device=self.device)
+            if self.ws.get("basic") is None or self.ws["basic"].numel() < nbytes:
+                self.ws["basic"] = torch.zeros(max(nbytes, 256), dtype=torch.uint8, device=self.device)
         ws = self.ws["basic"]
         rc = lib.cluster_qk_basic(ctypes.byref(p), _ptr(Q), _ptr(K), _ptr(V), _ptr(noise_q), _ptr(noise_k),
                                   int(iterations), _ptr(self.A_q), _ptr(self.A_k), _ptr(self.perm_q),
@@ -376,9 +396,10 @@ class Plan:
             _require_cuda(t, name)
         pr = self.problem
         if getattr(self, "block_idx_ragged", None) is None:
-            self.block_idx_ragged = torch.empty((pr.batch, pr.heads, pr.n_qc, pr.n_kc), dtype=torch.int32,
-                                                device=self.device)
-            self.keep_count = torch.empty((pr.batch, pr.heads, pr.n_qc), dtype=torch.int32, device=self.device)
+            with _on(stream):
+                self.block_idx_ragged = torch.empty((pr.batch, pr.heads, pr.n_qc, pr.n_kc), dtype=torch.int32,
+                                                    device=self.device)
+                self.keep_count = torch.empty((pr.batch, pr.heads, pr.n_qc), dtype=torch.int32, device=self.device)
         ws = self.ws["select"]
         rc = lib.select_blocks_adaptive(ctypes.byref(pr), _ptr(cq), _ptr(ck), _ptr(count_k), float(recall),
                                         int(min_count), _ptr(self.block_idx_ragged), _ptr(self.keep_count),
@@ -409,7 +430,7 @@ class Plan:
         """Q and K turned by their positions (rotary_axes), in buffers of the plan."""
         p, dt = self.problem, torch_dtype(self.problem)
         if getattr(self, "Qr", None) is None:
-            with _SAME if stream is None else torch.cuda.stream(stream):         # in order with what the call's stream does
+            with _on(stream):
                 self.Qr = torch.empty((p.batch, p.heads, p.n_q, p.head_dim), dtype=dt, device=self.device)
                 self.Kr = torch.empty((p.batch, p.heads, p.n_k, p.head_dim), dtype=dt, device=self.device)
         if positions_k is None and p.n_q == p.n_k:
@@ -515,9 +536,6 @@ def _call(fn, what: str, device: torch.device, stream: Optional[torch.cuda.Strea
         _check(rc, what)
 
 
-_SAME = contextlib.nullcontext()
-
-
 class Rotary:
     """Rotary positions: pairs[a] pairs of channels turn with axis a of a position, by `frequencies` (radians
     per step, one for every pair), or theta ** (-i / pairs[a]) for pair i of an axis.  adjacent: pair c is
@@ -571,8 +589,8 @@ def rotary_axes(rotary: Rotary, q, k, positions, inverse: bool = False, out_q=No
     if k is not None and out_k is not None:
         d = _rows(out_k, "out_k", shape_k, dtype, device)
     if c is None or (k is not None and d is None):
-        # new dense memory, in order with what the call's stream does
-        with _SAME if stream is None else torch.cuda.stream(stream):
+        # new dense memory
+        with _on(stream):
             if c is None:
                 out_q = q.new_empty(shape)
                 c = CaRows(out_q.data_ptr(), H * n * D, n * D, D)
@@ -619,6 +637,7 @@ class PagedCache:
         self.O = torch.zeros((p.batch, p.heads_q, 1, p.head_dim), dtype=self.dtype, device=dev)
         self.lse = torch.zeros((p.batch, p.heads_q, 1), dtype=torch.float32, device=dev)
         self.ws = torch.zeros(size.value, dtype=torch.uint8, device=dev)
+        _filled(dev)
 
     # the tensors of the cache: written into by the program, and the same ones for the life of the cache
     K_pages = property(lambda self: self._K_pages)
@@ -682,6 +701,7 @@ class WindowPlan:
         self.O = torch.zeros((p.batch, p.heads_q, p.n_q, p.head_dim), dtype=self.dtype, device=dev)
         self.lse = torch.zeros((p.batch, p.heads_q, p.n_q), dtype=torch.float32, device=dev)
         self.ws = torch.zeros(size.value, dtype=torch.uint8, device=dev)
+        _filled(dev)
 
     def window_attention_fwd(self, Q, K, V, len_q=None, len_k=None, out=None, want_lse: bool = True, stream=None):
         """window_attention_fwd of the C library.  Returns (O, lse or None): the plan's buffers, O or `out`; rows

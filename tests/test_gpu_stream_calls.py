@@ -1,0 +1,84 @@
+"""Calls for streams of tokens beside one another and beside other work."""
+import pytest
+import torch
+
+from paper_2608_26965_b200 import binding
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+def generator(seed):
+    g = torch.Generator(device=DEV)
+    g.manual_seed(seed)
+    return g
+
+
+def busy():
+    """Some tens of milliseconds of work on the current stream."""
+    torch.cuda._sleep(100_000_000)
+
+
+def on_a_side_stream(make, call, want):
+    """`call` on another stream right behind `make`, which has buffers filled on a busy one: what it gives is not touched afterwards."""
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    busy()
+    handle = make()
+    got = call(handle, side)
+    side.synchronize()
+    first = [x.clone() for x in got]
+    torch.cuda.synchronize()
+    for x, y, z in zip(first, got, want):
+        assert torch.equal(x, z) and torch.equal(y, z)
+
+
+def test_a_plan_is_ready_for_any_stream():
+    g = generator(1)
+    n, d = 700, 64
+    q, k, v = (torch.randn((1, h, n, d), generator=g, device=DEV).to(torch.bfloat16) for h in (4, 2, 2))
+    problem = binding.make_window_problem(1, 4, 2, n, n, d, "bf16", 60, 0, 4)
+    make = lambda: binding.WindowPlan(problem, DEV)
+    call = lambda plan, stream: plan.window_attention_fwd(q, k, v, stream=stream)
+    on_a_side_stream(make, call, [x.clone() for x in call(make(), None)])
+
+
+@pytest.mark.parametrize("per", [4, 300])
+def test_a_cache_is_ready_for_any_stream(per):
+    g = generator(2)
+    n, d = 60, 64
+    k, v = (torch.randn((1, 2, n, d), generator=g, device=DEV).to(torch.bfloat16) for _ in range(2))
+    q = torch.randn((1, 4, 1, d), generator=g, device=DEV).to(torch.bfloat16)
+    table = torch.arange(per, device=DEV).flip(0).reshape(1, per).int().contiguous()
+    problem = binding.make_cache_problem(1, 4, 2, d, "bf16", 16, per, per)
+
+    def call(cache, stream):
+        cache.cache_append(k, v, stream=stream)
+        return cache.paged_attention_fwd(q, appended=n, stream=stream) + (cache.K_pages, cache.V_pages)
+
+    make = lambda: binding.PagedCache(problem, DEV, page_table=table)
+    on_a_side_stream(make, call, [x.clone() for x in call(make(), None)])
+
+
+@pytest.mark.parametrize("path", ["forward", "adaptive", "basic", "rotary"])
+def test_a_clustering_plan_is_ready_for_any_stream(path):
+    g = generator(3)
+    n, d = 700, 64
+    q, k, v = (torch.randn((1, 2, n, d), generator=g, device=DEV) for _ in range(3))
+    pos = torch.arange(n, dtype=torch.int32, device=DEV).view(1, n, 1)
+    problem = binding.make_problem(1, 2, n, n, d, "fp32", 64, 64, 4)
+    make = lambda: binding.Plan(problem, DEV)
+    rows_q, rows_k, _ = make().basic_noise_rows()
+    noise = [torch.randn((1, 2, r, d), generator=g, device=DEV) for r in (rows_q, rows_k)]
+
+    def call(plan, stream):
+        if path == "adaptive":
+            return plan.forward_adaptive(q, k, v, 0.7, want_lse=True, stream=stream)
+        if path == "basic":
+            plan.cluster_qk_basic(q, k, v, *noise, stream=stream)
+            plan.select_blocks(stream=stream)
+            return plan.cluster_attention_fwd(stream=stream)
+        args = dict(rotary=binding.Rotary(d, [16]), positions_q=pos) if path == "rotary" else {}
+        return (plan.forward(q, k, v, stream=stream, **args),)
+
+    on_a_side_stream(make, call, [x.clone() for x in call(make(), None)])
