@@ -333,7 +333,8 @@ typedef struct {
   float softmax_scale;          /* 0 selects 1/sqrt(head_dim) */
 } ca_cache_t;
 
-/* Bytes of workspace of the two calls below (one workspace serves both, one call at a time). */
+/* Bytes of workspace of the two calls below (one workspace serves both, one call at a time).  Its first 256 bytes are set to
+ * zero by the caller before the first call. */
 int ca_cache_workspace_bytes(const ca_cache_t* c, size_t* bytes);
 
 /*
@@ -341,8 +342,9 @@ int ca_cache_workspace_bytes(const ca_cache_t* c, size_t* bytes);
  * NULL: all n) of K and V [batch, heads_kv, n, head_dim] go to rows lengths[b] + i.  K is turned by `rot` at
  * `positions` on the way (rot NULL: as it is).  lengths [batch], count [batch], page_table
  * [batch, pages_per_sequence] int32 (device) are only read.  A page that rows are put into belongs to one
- * sequence.  A row whose place is out of range (a page that the pool or the table does not have, a negative length, a
- * count that is not in 0 .. n) is left out and CA_ERR_BAD_INDEX recorded.
+ * sequence.  A row whose place is out of range (a page that the pool or the table does not have, a negative length)
+ * is left out, a count that is not in 0 .. n cut to it, and CA_ERR_BAD_INDEX recorded: attention calls on the same
+ * workspace report it too, until the next append.
  */
 int cache_append(const ca_cache_t* c, int32_t n, const ca_rows_t* K, const ca_rows_t* V,
                  const int32_t* lengths, const int32_t* count, const int32_t* page_table,
@@ -357,7 +359,7 @@ int cache_append(const ca_cache_t* c, int32_t n, const ca_rows_t* K, const ca_ro
  * are visible.  O [batch, heads_q, 1, head_dim] = softmax-weighted mean of their values, lse
  * [batch, heads_q] fp32 or NULL = log-sum-exp of their logits; without a visible row zeros and -inf.
  * What is not visible is not read.  A length out of range is cut to the range, a page out of range read as zero
- * keys and values, and CA_ERR_BAD_INDEX recorded.  The result does not depend on how the GPU schedules the parts.
+ * keys and values, and CA_ERR_BAD_INDEX recorded (also where the last append on this workspace recorded it).  The result does not depend on how the GPU schedules the parts.
  */
 int paged_attention_fwd(const ca_cache_t* c, const ca_rows_t* Q, const void* K_pages, const void* V_pages,
                         const int32_t* lengths, int32_t appended, const int32_t* page_table,
@@ -392,7 +394,8 @@ int window_attention_fwd(const ca_window_t* p, const ca_rows_t* Q, const ca_rows
                          const int32_t* len_q, const int32_t* len_k, const ca_rows_t* O, float* lse,
                          void* ws, size_t ws_bytes, void* stream);
 
-/* Reads the status word of a workspace as the last call on it left it (synchronises the device). */
+/* Reads the status word of a workspace as the last call on it left it (synchronises the device).  An error of
+ * cache_append stays there through the attention calls behind it. */
 int ca_last_status(const void* ws);
 
 /* Statistics of an attention workspace (synchronises the device): how many query clusters the

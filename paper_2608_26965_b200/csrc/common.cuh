@@ -18,6 +18,7 @@ namespace ca {
 constexpr size_t kStatusBytes = 256;
 constexpr size_t kStatusClearBytes = 252;
 constexpr int kTileWord = 1;
+constexpr int kAppendWord = 62;          // (a cache's workspace) status of the last append, which later calls leave as it is
 constexpr int kRecomputedWord = 63;
 
 extern std::atomic<unsigned long long> g_kernel_launches;   // kernels enqueued since the library was loaded

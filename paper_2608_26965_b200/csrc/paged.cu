@@ -102,6 +102,11 @@ __global__ void __launch_bounds__(1024) paged_plan_kernel(const __grid_constant_
   }
 }
 
+// What the append before left out is missing here: its error stays until the next append.
+__device__ __forceinline__ void write_status(const PagedParams& prm, int bad) {
+  prm.status[0] = bad || prm.status[kAppendWord] == CA_ERR_BAD_INDEX ? CA_ERR_BAD_INDEX : CA_OK;
+}
+
 template <int THREADS>
 __device__ __forceinline__ int bad_lengths(const PagedParams& prm) {
   int bad = 0;
@@ -808,7 +813,7 @@ __global__ void __launch_bounds__(kPagedThreads, W::CTAS) paged_kernel(const __g
       if (read) bad |= (unsigned)prm.page_table[e] >= (unsigned)prm.pages;
     }
     bad = __syncthreads_or(bad);
-    if (threadIdx.x == 0) *prm.status = bad ? CA_ERR_BAD_INDEX : CA_OK;
+    if (threadIdx.x == 0) write_status(prm, bad);
   }
 }
 
@@ -829,7 +834,7 @@ __global__ void __launch_bounds__(kJoinThreads, 3) paged_join_kernel(const __gri
     int bad = bad_lengths<kJoinThreads>(prm);
     for (int c = threadIdx.x; c < ctas; c += kJoinThreads) bad |= prm.bad[c];
     bad = __syncthreads_or(bad);
-    if (threadIdx.x == 0) *prm.status = bad ? CA_ERR_BAD_INDEX : CA_OK;
+    if (threadIdx.x == 0) write_status(prm, bad);
   }
   Units u;
   if (prm.planned) u = Units{prm.units[prm.batch], prm.units[b], (int)(prm.units[b + 1] - prm.units[b])};

@@ -198,7 +198,7 @@ __global__ void __launch_bounds__(256) rotary_kernel(const __grid_constant__ Rot
       else bad |= (unsigned)prm.page_table[(size_t)s * prm.pages_per_sequence + page] >= (unsigned)prm.pages;
     }
     bad = __syncthreads_or(bad);
-    if (threadIdx.x == 0) *prm.status = bad ? CA_ERR_BAD_INDEX : CA_OK;
+    if (threadIdx.x == 0) prm.status[0] = prm.status[kAppendWord] = bad ? CA_ERR_BAD_INDEX : CA_OK;
   }
 }
 

@@ -82,3 +82,35 @@ def test_a_clustering_plan_is_ready_for_any_stream(path):
         return (plan.forward(q, k, v, stream=stream, **args),)
 
     on_a_side_stream(make, call, [x.clone() for x in call(make(), None)])
+
+
+def cache_of(B, hq, kv, d, dtype, per, page_rows=16, **kw):
+    table = torch.arange(B * per, device=DEV).flip(0).reshape(B, per).int().contiguous()
+    return binding.PagedCache(binding.make_cache_problem(B, hq, kv, d, dtype, page_rows, B * per, per, **kw), DEV, page_table=table)
+
+
+@pytest.mark.parametrize("per", [2, 40])
+@pytest.mark.parametrize("batch", [3, 300])
+def test_the_error_of_an_append_outlives_the_attention_behind_it(per, batch):
+    """Until the next append, in caches of few rows and of many, of few sequences and of many."""
+    g = generator(per)
+    cache = cache_of(batch, 4, 2, 64, "bf16", per)
+    k, v = (torch.randn((batch, 2, 5, 64), generator=g, device=DEV).to(torch.bfloat16) for _ in range(2))
+    q = torch.randn((batch, 4, 1, 64), generator=g, device=DEV).to(torch.bfloat16)
+    count = torch.full((batch,), 5, dtype=torch.int32, device=DEV)
+    cache.paged_attention_fwd(q)
+    assert cache.last_status() == 0                         # (no append so far)
+    cache.cache_append(k, v, count=count)
+    cache.paged_attention_fwd(q, appended=5)
+    assert cache.last_status() == 0
+    for bad in (6, -1):
+        count[batch - 1] = bad
+        cache.cache_append(k, v, count=count)
+        for _ in range(2):
+            cache.paged_attention_fwd(q, appended=5)
+            assert cache.last_status() == binding.CA_ERR_BAD_INDEX
+        count[batch - 1] = 5
+        cache.cache_append(k, v, count=count)
+        assert cache.last_status() == 0
+        cache.paged_attention_fwd(q, appended=5)
+        assert cache.last_status() == 0
