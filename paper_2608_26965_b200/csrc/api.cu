@@ -12,6 +12,25 @@ using namespace ca;
 namespace ca {
 std::atomic<unsigned long long> g_kernel_launches{0};
 
+cudaError_t allow_smem(const void* kernel, size_t bytes) {
+  struct Known {
+    const void* kernel;
+    size_t bytes;
+  };
+  static std::mutex lock;
+  static Known known[256];                   // (a hundred kernels; of one that finds no place the limit is just set)
+  static int count = 0;
+  std::lock_guard<std::mutex> hold(lock);
+  int i = 0;
+  while (i < count && known[i].kernel != kernel) ++i;
+  if (i == count && count < 256) known[count++] = Known{kernel, 0};
+  const size_t most = i < count && known[i].bytes > bytes ? known[i].bytes : bytes;
+  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)most);
+  if (e != cudaSuccess) (void)cudaGetLastError();
+  else if (i < count) known[i].bytes = most;
+  return e;
+}
+
 // ---- per-kernel-group timers (off unless ca_profile(1) was called) ------------------------------
 namespace {
 constexpr int kProfPairs = 512;

@@ -368,7 +368,7 @@ static int launch_rows(const ca_problem_t& pr, const T* Qp, const T* Kp, const T
   const dim3 grid = redo ? dim3(ceil_div(n_clusters, per_cta))
                          : dim3(n_qc * ceil_div(pr.cluster_q, QR), pr.batch * pr.heads);
   auto k = attn_ref_kernel<T, D, QR, RY, KT, direct, many>;
-  CA_RETURN_IF_CUDA(cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+  CA_RETURN_IF_CUDA(allow_smem(k, smem));
   launch_chained(k, grid, NT, smem, st, Qp, Kp, Vp, ck, cv, count_k, block_idx, keep_count, list_stride, perm_q, pr.n_q, pr.n_k,
                                 pr.cluster_q, pr.cluster_k, pr.keep, pr.compensate, scale, O, lse, status, redo,
                                 redo_tiles, redo_count, per_cta, n_clusters);

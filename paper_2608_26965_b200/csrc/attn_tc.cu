@@ -1159,7 +1159,7 @@ static int launch_tc_d(const CUtensorMap* maps, const TcParams& prm, int grid, L
   static_assert(1024 + C::OFF_BITMAP + 4 * (MODE == kPairs ? 2 * kPairBitmapWords : kBitmapWords) <= 227 * 1024, "bitmaps of the largest number of key clusters");
   const size_t smem = 1024 + C::OFF_BITMAP + (size_t)prm.bitmap_words * 4 * (MODE == kPairs ? 2 : 1);
   auto k = attn_tc_kernel<D, F8, MODE>;
-  CA_RETURN_IF_CUDA(cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+  CA_RETURN_IF_CUDA(allow_smem(k, smem));
   launch_chained(k, grid, kTcThreads, smem, st, maps[0], maps[1], maps[2], maps[3], maps[4], prm);
   CA_LAUNCH_CHECK();
   return CA_OK;

@@ -76,6 +76,12 @@ inline void launch_chained(void (*kernel)(Params...), dim3 grid, dim3 block, siz
   (void)cudaLaunchKernelEx(&cfg, kernel, Params(args)...);      // CA_LAUNCH_CHECK picks up an error
 }
 
+// Dynamic shared memory that a launch of `kernel` may ask for: `bytes`, or more where another call has asked for more (the limit is the
+// kernel's, and a host thread that lowered it would fail the launch that another one is about to make).
+cudaError_t allow_smem(const void* kernel, size_t bytes);
+template <typename... Params>
+inline cudaError_t allow_smem(void (*kernel)(Params...), size_t bytes) { return allow_smem(reinterpret_cast<const void*>(kernel), bytes); }
+
 // Multiprocessors of the current device, asked for once per device (0 on error).
 inline int multiprocessors(int* device = nullptr) {
   static std::atomic<int> known[64];

@@ -191,7 +191,7 @@ int launch_cholesky_factor(const double* gram, const double* sum, double n, doub
   __nv_bfloat16* lo = static_cast<__nv_bfloat16*>(wt_lo);
   const size_t smem = sizeof(double) * ((size_t)D * (D + 1) + 2 * kPanel * (D + 8) + D);
   auto k = D == 64 ? cholesky_factor_kernel<64> : cholesky_factor_kernel<128>;
-  CA_RETURN_IF_CUDA(cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+  CA_RETURN_IF_CUDA(allow_smem(k, smem));
   launch_chained(k, count, 4 * D, smem, st, gram, sum, n, scale, out64, out32, hi, lo);
   CA_LAUNCH_CHECK();
   return CA_OK;

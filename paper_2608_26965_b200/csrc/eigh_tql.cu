@@ -1137,7 +1137,7 @@ __global__ void __launch_bounds__(kThreads) eigh_tql_kernel(const PcaArgs a) {
 int launch_pca(const PcaArgs& args, int count, int D, LaunchStream st) {
   const size_t smem = sizeof(float) * ((size_t)3 * D * (D + 4) + 8 * D + 21 * D);
   auto k = D == 64 ? eigh_tql_kernel<64> : eigh_tql_kernel<128>;
-  CA_RETURN_IF_CUDA(cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+  CA_RETURN_IF_CUDA(allow_smem(k, smem));
   launch_chained(k, count, kThreads, smem, st, args);
   CA_LAUNCH_CHECK();
   return CA_OK;

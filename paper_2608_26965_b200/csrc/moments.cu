@@ -229,11 +229,11 @@ static int launch_transform_t(const T* X, int problems, int n_rows, int D, const
   size_t smem = (size_t)(D * D + 64 * (D + 4)) * sizeof(float);
   if (D == 64) {
     auto k = transform_rows_kernel<T, 64>;
-    CA_RETURN_IF_CUDA(cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    CA_RETURN_IF_CUDA(allow_smem(k, smem));
     launch_chained(k, grid, 256, smem, st, X, n_rows, W, bias, normalize, out);
   } else {
     auto k = transform_rows_kernel<T, 128>;
-    CA_RETURN_IF_CUDA(cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    CA_RETURN_IF_CUDA(allow_smem(k, smem));
     launch_chained(k, grid, 256, smem, st, X, n_rows, W, bias, normalize, out);
   }
   CA_LAUNCH_CHECK();

@@ -964,7 +964,7 @@ static int launch_paged_d(PagedParams& prm, LaunchStream st) {
   prm.row_tiles = ceil_div(prm.group, W::ROWS);
   const int smem = C::smem(prm.group);
   auto kernel = paged_kernel<W, D>;
-  CA_RETURN_IF_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+  CA_RETURN_IF_CUDA(allow_smem(kernel, smem));
   const long long pairs = (long long)prm.batch * prm.heads_kv * prm.row_tiles;
   prm.direct = (long long)prm.pages_per_sequence * prm.page_rows <= kDirectRows;
   if (prm.direct) {

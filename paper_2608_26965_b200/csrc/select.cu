@@ -400,7 +400,7 @@ static int launch_score_tiles(const float* cq, const float* ck, int P, int n_qc,
   const int rows = min(chunk_rows, n_qc - row0);
   const dim3 grid(ceil_div(n_kc, 64), ceil_div(rows, 64), P);
   const size_t smem = spread_smem((size_t)2 * D * 64 * sizeof(float), 0, (long long)grid.x * grid.y * grid.z);
-  CA_RETURN_IF_CUDA(cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+  CA_RETURN_IF_CUDA(allow_smem(k, smem));
   launch_chained(k, grid, 256, smem, st, cq, ck, n_qc, n_kc, row0, chunk_rows, scores);
   CA_LAUNCH_CHECK();
   return CA_OK;
@@ -415,11 +415,11 @@ int launch_score_select(const float* cq, const float* ck, int P, int n_qc, int n
     dim3 grid(ceil_div(n_qc, kSelectQT), P);
     if (D == 64) {
       auto k = score_select_kernel<64, kSelectQT>;
-      CA_RETURN_IF_CUDA(cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+      CA_RETURN_IF_CUDA(allow_smem(k, smem));
       launch_chained(k, grid, kSelectThreads, smem, st, cq, ck, n_qc, n_kc, keep, block_idx, nullptr, 0, n_qc, status);
     } else {
       auto k = score_select_kernel<128, kSelectQT>;
-      CA_RETURN_IF_CUDA(cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+      CA_RETURN_IF_CUDA(allow_smem(k, smem));
       launch_chained(k, grid, kSelectThreads, smem, st, cq, ck, n_qc, n_kc, keep, block_idx, nullptr, 0, n_qc, status);
     }
     CA_LAUNCH_CHECK();
@@ -434,10 +434,10 @@ int launch_score_select(const float* cq, const float* ck, int P, int n_qc, int n
   auto k64 = score_select_kernel<64, 1>;
   auto k128 = score_select_kernel<128, 1>;
   if (by_warps) {
-    CA_RETURN_IF_CUDA(cudaFuncSetAttribute(select_rows_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    CA_RETURN_IF_CUDA(allow_smem(select_rows_kernel, smem));
   } else {
-    CA_RETURN_IF_CUDA(cudaFuncSetAttribute(k64, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
-    CA_RETURN_IF_CUDA(cudaFuncSetAttribute(k128, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    CA_RETURN_IF_CUDA(allow_smem(k64, smem));
+    CA_RETURN_IF_CUDA(allow_smem(k128, smem));
   }
   for (int row0 = 0; row0 < n_qc; row0 += chunk) {
     const int rows = min(chunk, n_qc - row0);
@@ -613,8 +613,8 @@ int launch_select_adaptive(const float* cq, const float* ck, const int32_t* coun
   const float c_log2 = scale * 1.4426950408889634f;      // one float32 product, as in the definition
   auto k64 = select_adaptive_kernel<64>;
   auto k128 = select_adaptive_kernel<128>;
-  CA_RETURN_IF_CUDA(cudaFuncSetAttribute(k64, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
-  CA_RETURN_IF_CUDA(cudaFuncSetAttribute(k128, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+  CA_RETURN_IF_CUDA(allow_smem(k64, smem));
+  CA_RETURN_IF_CUDA(allow_smem(k128, smem));
   for (int row0 = 0; row0 < n_qc; row0 += step) {
     const int rows = min(step, n_qc - row0);
     const float* scores = nullptr;

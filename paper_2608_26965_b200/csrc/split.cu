@@ -905,7 +905,7 @@ static int launch_level(SplitParams& prm, bool keys_in, int level, int max_seg, 
                               : (wide ? split_level_kernel<128, 1024, false> : split_level_kernel<128, 512, false>);
   prm.level = level;
   prm.smem_rows = per_cta < kSmemRowsMax ? per_cta : kSmemRowsMax;
-  CA_RETURN_IF_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemRowsMax * 8));
+  CA_RETURN_IF_CUDA(allow_smem(kernel, kSmemRowsMax * 8));
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((1u << level) * csize, prm.sides * prm.problems);
   cfg.blockDim = dim3(wide ? 1024 : 512);
@@ -979,7 +979,7 @@ int launch_split(const float* Yq, const float* Yk, int problems, int D, int n_q,
   const bool few = 2LL * slots * problems <= 296;          // both sides run at the same time
   auto tail_kernel = D == 64 ? (few ? split_tail_kernel<64, 512> : split_tail_kernel<64, 256>)
                              : (few ? split_tail_kernel<128, 512> : split_tail_kernel<128, 256>);
-  CA_RETURN_IF_CUDA(cudaFuncSetAttribute(tail_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(TailSmem)));
+  CA_RETURN_IF_CUDA(allow_smem(tail_kernel, sizeof(TailSmem)));
   launch_chained(tail_kernel, dim3(slots, prm.sides * problems), few ? 512 : 256, sizeof(TailSmem), st, prm);
   CA_LAUNCH_CHECK();
   return CA_OK;
@@ -1767,11 +1767,11 @@ static int launch_split_basic_t(const T* Q, const T* K, const float* A_q, const 
     const size_t dsmem = (size_t)2 * D * (D + 4) * sizeof(float);
     if (D == 64) {
       auto dk = basic_direction_kernel<T, 64>;
-      CA_RETURN_IF_CUDA(cudaFuncSetAttribute(dk, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)dsmem));
+      CA_RETURN_IF_CUDA(allow_smem(dk, dsmem));
       launch_chained(dk, dim3(1u << level, 2 * problems), 64, dsmem, st, bp);
     } else {
       auto dk = basic_direction_kernel<T, 128>;
-      CA_RETURN_IF_CUDA(cudaFuncSetAttribute(dk, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)dsmem));
+      CA_RETURN_IF_CUDA(allow_smem(dk, dsmem));
       launch_chained(dk, dim3(1u << level, 2 * problems), 128, dsmem, st, bp);
     }
     CA_LAUNCH_CHECK();
@@ -1790,11 +1790,11 @@ static int launch_split_basic_t(const T* Q, const T* K, const float* A_q, const 
   const int slots = 1 << top;
   if (D == 64) {
     auto tk = basic_tail_kernel<T, 64>;
-    CA_RETURN_IF_CUDA(cudaFuncSetAttribute(tk, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(BasicTailSmem<64>)));
+    CA_RETURN_IF_CUDA(allow_smem(tk, sizeof(BasicTailSmem<64>)));
     launch_chained(tk, dim3(slots, 2 * problems), kSplitThreads, sizeof(BasicTailSmem<64>), st, bp, prm);
   } else {
     auto tk = basic_tail_kernel<T, 128>;
-    CA_RETURN_IF_CUDA(cudaFuncSetAttribute(tk, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(BasicTailSmem<128>)));
+    CA_RETURN_IF_CUDA(allow_smem(tk, sizeof(BasicTailSmem<128>)));
     launch_chained(tk, dim3(slots, 2 * problems), kSplitThreads, sizeof(BasicTailSmem<128>), st, bp, prm);
   }
   CA_LAUNCH_CHECK();

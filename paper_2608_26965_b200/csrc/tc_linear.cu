@@ -691,7 +691,7 @@ int launch_gram_tc(const void* X, int problems, int n_rows, int D, float* partia
   CUtensorMap mx;
   if (!map_3d(&mx, X, problems, n_rows, D, 2, 64, kRows)) return CA_ERR_CUDA;
   auto k = D == 64 ? gram_tc_kernel<64> : gram_tc_kernel<128>;
-  CA_RETURN_IF_CUDA(cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+  CA_RETURN_IF_CUDA(allow_smem(k, smem));
   launch_chained(k, dim3(prm.n_chunks, problems), kLinThreads, smem, st, mx, prm);
   CA_LAUNCH_CHECK();
   return launch_gram_finalize(partial, problems, prm.n_chunks, D, gram, colsum, st);
@@ -709,7 +709,7 @@ static int launch_rep_gram(const void* X, int problems, int n_rows, int normaliz
       !map_2d(&mwl, wt_lo, (size_t)problems * D, D, D))
     return CA_ERR_CUDA;
   auto k = rep_gram_tc_kernel<D>;
-  CA_RETURN_IF_CUDA(cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM));
+  CA_RETURN_IF_CUDA(allow_smem(k, C::SMEM));
   launch_chained(k, dim3(prm.n_chunks, problems), C::THREADS, C::SMEM, st, mx, mwh, mwl, prm);
   CA_LAUNCH_CHECK();
   return launch_gram_finalize(partial, problems, prm.n_chunks, D, gram, colsum, st);
@@ -741,7 +741,7 @@ int launch_transform_tc(const void* X, int problems, int n_rows, int D, const fl
     return CA_ERR_CUDA;
   const size_t smem = 1024 + (size_t)fixed + (size_t)prm.stages * tile + D * 4;
   auto k = D == 64 ? transform_tc_kernel<64> : transform_tc_kernel<128>;
-  CA_RETURN_IF_CUDA(cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+  CA_RETURN_IF_CUDA(allow_smem(k, smem));
   launch_chained(k, dim3(ceil_div(total_tiles, prm.tiles_per_cta), problems), kLinThreads, smem, st, mx, mwh, mwl, mo, prm);
   CA_LAUNCH_CHECK();
   return CA_OK;

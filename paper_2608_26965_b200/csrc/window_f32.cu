@@ -234,7 +234,7 @@ __global__ void __launch_bounds__(kWfThreads) window_f32_kernel(const __grid_con
 template <int D>
 static int launch_window_f32_d(const WindowParams& prm, LaunchStream st) {
   auto kernel = window_f32_kernel<D>;
-  CA_RETURN_IF_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, WfCfg<D>::SMEM));
+  CA_RETURN_IF_CUDA(allow_smem(kernel, WfCfg<D>::SMEM));
   const long long n_work = (long long)ceil_div(prm.n_q, kWfRows) * prm.heads_q * prm.batch;
   if (n_work > 0x7fffffffLL) return CA_ERR_UNSUPPORTED;
   launch_chained(kernel, (unsigned)n_work, kWfThreads, WfCfg<D>::SMEM, st, prm);

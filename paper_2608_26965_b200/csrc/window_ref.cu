@@ -251,7 +251,7 @@ template <typename T, int D, int M>
 static int launch_window_ref_m(const WindowParams& prm, LaunchStream st) {
   using C = WrCfg<D, M>;
   auto kernel = window_ref_kernel<T, D, M>;
-  CA_RETURN_IF_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM));
+  CA_RETURN_IF_CUDA(allow_smem(kernel, C::SMEM));
   const long long n_work = (long long)ceil_div(prm.n_q, M) * prm.heads_q * prm.batch;
   // a CTA for every tile of rows; to compute rows again, hardly ever any, one to an SM
   const long long most = prm.redo ? 148 : 0x7fffffffLL;

@@ -703,7 +703,7 @@ static int launch_window_tc_d(const CUtensorMap* maps, const WtParams& prm, int 
   auto kernel = window_tc_kernel<D>;
   const int sms = multiprocessors();
   if (sms == 0) return CA_ERR_CUDA;
-  CA_RETURN_IF_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, WtCfg<D>::SMEM));
+  CA_RETURN_IF_CUDA(allow_smem(kernel, WtCfg<D>::SMEM));
   launch_chained(kernel, n_work < sms ? n_work : sms, kWtThreads, WtCfg<D>::SMEM, st, maps[0], maps[1], maps[2], prm);
   CA_LAUNCH_CHECK();
   return CA_OK;

@@ -1,4 +1,6 @@
 """Calls for streams of tokens beside one another and beside other work."""
+import threading
+
 import pytest
 import torch
 
@@ -114,3 +116,39 @@ def test_the_error_of_an_append_outlives_the_attention_behind_it(per, batch):
         assert cache.last_status() == 0
         cache.paged_attention_fwd(q, appended=5)
         assert cache.last_status() == 0
+
+
+def test_host_threads_call_the_same_kernels_at_other_sizes():
+    """Shared memory of a launch goes by the heads that share a key head, by the number of clusters, by the rows."""
+    d, calls = 64, []
+    g = generator(5)
+    for group in (1, 8, 3):
+        cache = cache_of(4, group, 1, d, "bf16", 40)
+        k, v, q = (torch.randn((4, h, n, d), generator=g, device=DEV).to(torch.bfloat16) for h, n in ((1, 300), (1, 300), (group, 1)))
+        cache.cache_append(k, v)
+        calls.append((lambda stream, c=cache, q=q: c.paged_attention_fwd(q, appended=300, stream=stream)[0], cache))
+    for n in (600, 9000, 3000):
+        plan = binding.Plan(binding.make_problem(1, 1, n, n, d, "bf16", 64, 64, 4), DEV)
+        q, k, v = (torch.randn((1, 1, n, d), generator=g, device=DEV).to(torch.bfloat16) for _ in range(3))
+        calls.append((lambda stream, p=plan, x=(q, k, v): p.forward(*x, stream=stream), plan))
+    want = [call(None).clone() for call, _ in calls]
+    streams = [torch.cuda.Stream() for _ in calls]
+    torch.cuda.synchronize()
+    failed, got = [], [None] * len(calls)
+
+    def work(i):
+        try:
+            for _ in range(60):
+                got[i] = calls[i][0](streams[i])
+        except Exception as e:  # noqa: BLE001
+            failed.append((i, e))
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(len(calls))]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    assert not failed
+    for x, y in zip(got, want):
+        assert torch.equal(x, y)
