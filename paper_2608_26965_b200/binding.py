@@ -224,10 +224,19 @@ def torch_dtype(problem: CaProblem) -> torch.dtype:
     return torch.bfloat16 if problem.dtype == CA_DTYPE_BF16 else torch.float32
 
 
+def _numbers32(**numbers) -> None:
+    """ctypes takes the lower 32 bits of what does not fit an int32 without a word: a left bound of 2^32 would be one of 0."""
+    for name, x in numbers.items():
+        if not -2 ** 31 <= x < 2 ** 31:
+            raise ClusterAttnError(f"{name} must be a 32-bit number, not {x}")
+
+
 def make_problem(batch: int, heads: int, n_q: int, n_k: int, head_dim: int, dtype: str, cluster_q: int,
                  cluster_k: int, keep: int, compensate: bool = True, softmax_scale: float = 0.0,
                  flags: int = 0) -> CaProblem:
     code = {"fp32": CA_DTYPE_FP32, "bf16": CA_DTYPE_BF16}[dtype]
+    _numbers32(batch=batch, heads=heads, n_q=n_q, n_k=n_k, head_dim=head_dim, cluster_q=cluster_q, cluster_k=cluster_k, keep=keep,
+               flags=flags)
     return CaProblem(batch, heads, n_q, n_k, head_dim, code, cluster_q, cluster_k, keep,
                      1 if compensate else 0, float(softmax_scale), flags)
 
@@ -604,6 +613,8 @@ def rotary_axes(rotary: Rotary, q, k, positions, inverse: bool = False, out_q=No
 
 def make_cache_problem(batch: int, heads_q: int, heads_kv: int, head_dim: int, dtype: str, page_rows: int, pages: int,
                        pages_per_sequence: int, left: int = -1, sinks: int = 0, softmax_scale: float = 0.0) -> CaCache:
+    _numbers32(batch=batch, heads_q=heads_q, heads_kv=heads_kv, head_dim=head_dim, page_rows=page_rows, pages=pages,
+               pages_per_sequence=pages_per_sequence, left=left, sinks=sinks)
     return CaCache(batch, heads_q, heads_kv, head_dim, _code(dtype), page_rows, pages, pages_per_sequence, left, sinks,
                    float(softmax_scale))
 
@@ -671,6 +682,7 @@ class PagedCache:
         rows.  Returns (O, lse [batch, heads_q, 1] or None): the cache's buffers, O or `out`."""
         p = self.problem
         shape = (p.batch, p.heads_q, 1, p.head_dim)
+        _numbers32(appended=appended)
         out = self.O if out is None else out
         q, o = _rows(Q, "Q", shape, self.dtype, self.device), _rows(out, "out", shape, self.dtype, self.device)
         lse = self.lse if want_lse else None
@@ -686,6 +698,8 @@ class PagedCache:
 
 def make_window_problem(batch: int, heads_q: int, heads_kv: int, n_q: int, n_k: int, head_dim: int, dtype: str, left: int,
                         right: int, sinks: int = 0, softmax_scale: float = 0.0, flags: int = 0) -> CaWindow:
+    _numbers32(batch=batch, heads_q=heads_q, heads_kv=heads_kv, n_q=n_q, n_k=n_k, head_dim=head_dim, left=left, right=right, sinks=sinks,
+               flags=flags)
     return CaWindow(batch, heads_q, heads_kv, n_q, n_k, head_dim, _code(dtype), left, right, sinks, float(softmax_scale), flags)
 
 
