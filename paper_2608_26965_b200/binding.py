@@ -448,10 +448,17 @@ class Plan:
         rotary_axes(rotary, K, None, positions_k, out_q=self.Kr, stream=stream)
         return self.Qr, self.Kr
 
+    @staticmethod
+    def _no_positions(positions_q, positions_k):
+        if positions_q is not None or positions_k is not None:
+            raise ClusterAttnError("positions without rotary")
+
     def forward_adaptive(self, Q, K, V, recall: float, min_count: int = 16, want_lse=False, stream=None, rotary=None,
                          positions_q=None, positions_k=None):
         if rotary is not None:
             Q, K = self._turned(Q, K, rotary, positions_q, positions_k, stream)
+        else:
+            self._no_positions(positions_q, positions_k)
         self.cluster_qk(Q, K, V, stream=stream)
         self.select_blocks_adaptive(recall, min_count, stream=stream)
         return self.cluster_attention_fwd_ragged(want_lse=want_lse, stream=stream)
@@ -462,6 +469,8 @@ class Plan:
         queries' own); Q and K may then be strided."""
         if rotary is not None:
             Q, K = self._turned(Q, K, rotary, positions_q, positions_k, stream)
+        else:
+            self._no_positions(positions_q, positions_k)
         self.cluster_qk(Q, K, V, stream=stream)
         self.select_blocks(stream=stream)
         return self.cluster_attention_fwd(want_lse=want_lse, stream=stream)[0]

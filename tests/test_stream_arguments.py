@@ -20,3 +20,13 @@ def test_numbers_beyond_32_bits_are_refused(big):
     none.problem = binding.make_cache_problem(**cache)
     with pytest.raises(binding.ClusterAttnError, match="appended"):
         none.paged_attention_fwd(None, appended=big)
+
+
+def test_positions_without_rotary_are_refused():
+    """They would be left aside without a word."""
+    plan = object.__new__(binding.Plan)
+    for args in (dict(positions_q=1), dict(positions_k=1)):
+        with pytest.raises(binding.ClusterAttnError, match="positions without rotary"):
+            plan.forward(None, None, None, **args)
+        with pytest.raises(binding.ClusterAttnError, match="positions without rotary"):
+            plan.forward_adaptive(None, None, None, 0.5, **args)
