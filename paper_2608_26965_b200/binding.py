@@ -280,7 +280,7 @@ class Plan:
         if not torch.cuda.is_available():
             raise ClusterAttnError("no CUDA device: libclusterattn has no CPU path")
         load_library()
-        self.problem = problem
+        self.problem = problem = problem.copy()             # (the caller's may change; the buffers here do not)
         self.device = torch.device(device)
         p = problem
         dt = torch_dtype(p)
@@ -636,7 +636,7 @@ class PagedCache:
 
     def __init__(self, problem: CaCache, device: str = "cuda:0", K_pages=None, V_pages=None, page_table=None, lengths=None):
         self.device = dev = _cuda_device(device)
-        self.problem = p = problem
+        self.problem = p = CaCache.from_buffer_copy(problem)             # (as in Plan)
         lib = load_library()
         size = ctypes.c_size_t()
         _check(lib.ca_cache_workspace_bytes(ctypes.byref(p), ctypes.byref(size)), "ca_cache_workspace_bytes")
@@ -717,7 +717,7 @@ class WindowPlan:
 
     def __init__(self, problem: CaWindow, device: str = "cuda:0"):
         self.device = dev = _cuda_device(device)
-        self.problem = p = problem
+        self.problem = p = CaWindow.from_buffer_copy(problem)
         size = ctypes.c_size_t()
         _check(load_library().ca_window_workspace_bytes(ctypes.byref(p), ctypes.byref(size)), "ca_window_workspace_bytes")
         self.dtype = _TORCH[p.dtype]

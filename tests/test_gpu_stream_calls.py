@@ -152,3 +152,12 @@ def test_host_threads_call_the_same_kernels_at_other_sizes():
     assert not failed
     for x, y in zip(got, want):
         assert torch.equal(x, y)
+
+
+def test_a_problem_that_changes_does_not_change_what_was_made_for_it():
+    """A cache that took the caller's later number of pages for its own would read behind its pools."""
+    window, cache = binding.make_window_problem(1, 2, 2, 40, 40, 64, "bf16", 3, 0), binding.make_cache_problem(1, 2, 2, 64, "bf16", 16, 4, 4)
+    plan = binding.make_problem(1, 1, 64, 64, 64, "fp32", 16, 16, 2)
+    made = binding.WindowPlan(window, DEV), binding.PagedCache(cache, DEV), binding.Plan(plan, DEV)
+    window.n_q, cache.pages, cache.pages_per_sequence, plan.n_q = 400, 1000, 1000, 640
+    assert made[0].problem.n_q == 40 and made[1].problem.pages == made[1].problem.pages_per_sequence == 4 and made[2].problem.n_q == 64
