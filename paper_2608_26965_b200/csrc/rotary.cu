@@ -5,7 +5,8 @@
 //     (x, y) -> (x cos t - y sin t, x sin t + y cos t),          the inverse by -t.
 // Positions are whole numbers, so t / (2 pi) is only needed modulo 1: the host turns a frequency into a 64-bit
 // fraction of a turn, and the product with the position modulo 2^64 is the phase, to 2^-64 of a turn per step at any
-// distance, without a double in the kernel.
+// distance, without a double in the kernel.  The nearest quarter turn is taken off in whole numbers and the remainder rounded to fp32 once,
+// so that sines and cosines next to zero are as accurate as the others.
 //
 // What bounds it: memory.  Every element is read and written once in 16-byte vectors; a thread keeps the sines
 // and cosines of its channels and goes through heads with them, which share the positions of a row.
@@ -66,6 +67,22 @@ union Pack {
   T e[W];
   __device__ __forceinline__ Pack() {}
 };
+
+// Sine and cosine of a phase (2^64: a turn).  The quarter turn next to it is taken off; of the remainder r half turns, |r| <= 1/4,
+//     sin(pi r) = r (pi + t S(t)),  cos(pi r) = 1 + t C(t),  t = r^2
+// with polynomials fitted to the smallest relative error (of sine 0.06 u, of cosine 0.001 u, u = 2^-24), pi in two parts: with their roundings
+// 1.2 u and 1.4 u.  (sincospif of the remainder, which looks for the quarter again, cost 6 %: a video layer of 2 x 40 heads by 32,760 rows
+// 218 us instead of 205.)
+__device__ __forceinline__ void sine_cosine(unsigned long long phase, float* sine, float* cosine) {
+  const unsigned top = (unsigned)(phase >> 32), quarter = (top + 0x20000000u) >> 30;
+  const float r = fmaf((float)(unsigned)phase, 0x1p-63f, (float)(int)(top - (quarter << 30)) * 0x1p-31f), t = r * r;
+  const float S = fmaf(fmaf(-0.58947957f, t, 2.5498104f), t, -5.1677094f);
+  const float C = fmaf(fmaf(fmaf(0.23136422f, t, -1.3350506f), t, 4.0587077f), t, -4.934802f);
+  const float s = fmaf(r, 3.1415927f, r * fmaf(S, t, -8.7422777e-8f)), c = fmaf(C, t, 1.f);
+  const float x = quarter & 1 ? c : s, y = quarter & 1 ? s : c;
+  *sine = quarter & 2 ? -x : x;
+  *cosine = (quarter + 1) & 2 ? -y : y;
+}
 
 template <typename T>
 __device__ __forceinline__ void turn(T& x, T& y, float c, float s) {
@@ -135,7 +152,7 @@ __device__ __forceinline__ void rotary_rows(const unsigned long long* s_turns, c
       sn[i] = 0.f;
       if (pair < R) {
         const unsigned long long phase = (unsigned long long)(long long)pos[s_axis[pair]] * s_turns[pair];
-        sincospif((float)(long long)phase * 0x1p-63f, &sn[i], &cs[i]);
+        sine_cosine(phase, &sn[i], &cs[i]);
         if (prm.inverse) sn[i] = -sn[i];
         turned = i + 1;
       }
