@@ -21,7 +21,7 @@
  *   - The first 256 bytes of a workspace hold a status word that kernels set when
  *     a bounded wait expires (CA_ERR_TIMEOUT) or an index supplied by the caller
  *     is out of range (CA_ERR_BAD_INDEX); ca_last_status reads it.  Every call
- *     clears it on its stream before its kernels run.
+ *     clears it on its stream before its kernels run, or writes it in them.
  */
 #ifndef CLUSTER_ATTENTION_H_
 #define CLUSTER_ATTENTION_H_

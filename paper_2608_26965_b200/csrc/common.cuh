@@ -12,9 +12,10 @@ namespace ca {
 
 // Status block at the start of every workspace: word 0 is the status code (CA_OK or the first
 // error a kernel recorded), word kTileWord the counter that hands out tiles of the attention kernel;
-// every call clears the first kStatusClearBytes on its stream, by a memset or in its first kernel (which saves
-// 3 us: 4 heads of 512 rows in fp32 212 -> 208.5 us, 8 heads of 1,531 x 23,117 rows 328.5 -> 324).  The last word is a counter that calls
-// only add to (query clusters recomputed by the second attention pass).
+// calls of the clustering path clear the first kStatusClearBytes on their stream, by a memset or in their first kernel (which saves
+// 3 us: 4 heads of 512 rows in fp32 212 -> 208.5 us, 8 heads of 1,531 x 23,117 rows 328.5 -> 324); those for streams of tokens write the words
+// that they use, one block of threads each.  The last word is a counter that calls only add to (query clusters recomputed by the second
+// attention pass).
 constexpr size_t kStatusBytes = 256;
 constexpr size_t kStatusClearBytes = 252;
 constexpr int kTileWord = 1;

@@ -33,7 +33,9 @@ constexpr int kPagedThreads = kPagedWarps * 32;
 // What the start and the end of a (sequence, key head, row tile) cost, in units of rows: without it the parts that hold many short
 // sequences take longest (64 sequences of 1 to 8,192 rows, 8 key heads of 4 query heads, d = 128: 0 90 us, 1 61, 2 51.5, 4 53, 8 57).
 constexpr int kPairUnits = 3;
-// Caches of at most so many rows a sequence are not split: a CTA for every (sequence, key head, row tile), one launch instead of three.
+// Caches of at most so many rows a sequence are not split: a CTA for every (sequence, key head, row tile), one launch instead of two or three
+// (of 8, 64 and 256 sequences of up to 256 rows, 8 key heads of 4 query heads, d = 128, 7.0, 12.5 and 45 us instead of 10.0, 20 and 60; of
+// up to 512 rows 10.1, 18 and 62 instead of 9.9, 24 and 75, one sequence alone 11.1 instead of 8.6; fp32 and d = 64 alike).
 constexpr int kDirectRows = 256;
 constexpr int kAddUp = 256;                    // sequences whose lengths every CTA adds up by itself; of more, a launch does
 constexpr int kPagedMaxCtas = 640;           // most CTAs of a launch: the workspace holds two partial results of each

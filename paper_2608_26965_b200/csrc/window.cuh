@@ -23,7 +23,7 @@ constexpr int kWindowBlock = 256;   // two of them: what a CTA works on at a tim
 // words of the status block behind the status: a counter that hands out work, whether rows are to be computed again
 constexpr int kNextWord = kTileWord, kRedoWord = kTileWord + 1;
 
-// Lengths of a batch item, kept in range (what is out of it is flagged by check_lengths).
+// Lengths of a batch item, kept in range (what is out of it is flagged by window_status, or by the launch that prepares the bf16 kernel's).
 struct WindowItem {
   int len_q, len_k, shift;          // the last query stands at the last key: query i at key i + shift
   __device__ __forceinline__ WindowItem(const WindowParams& prm, int b) {

@@ -254,7 +254,8 @@ static int launch_window_ref_m(const WindowParams& prm, LaunchStream st) {
   CA_RETURN_IF_CUDA(allow_smem(kernel, C::SMEM));
   const long long n_work = (long long)ceil_div(prm.n_q, M) * prm.heads_q * prm.batch;
   // a CTA for every tile of rows; to compute rows again, hardly ever any, one to an SM
-  const long long most = prm.redo ? 148 : 0x7fffffffLL;
+  const long long most = prm.redo ? multiprocessors() : 0x7fffffffLL;
+  if (most == 0) return CA_ERR_CUDA;
   launch_chained(kernel, (unsigned)(n_work < most ? n_work : most), C::THREADS, C::SMEM, st, prm);
   CA_LAUNCH_CHECK();
   return CA_OK;
@@ -262,7 +263,7 @@ static int launch_window_ref_m(const WindowParams& prm, LaunchStream st) {
 
 template <typename T, int D>
 static int launch_window_ref_d(const WindowParams& prm, LaunchStream st) {
-  if (!prm.redo && (long long)ceil_div(prm.n_q, 64) * prm.heads_q * prm.batch < 148) return launch_window_ref_m<T, D, 32>(prm, st);
+  if (!prm.redo && (long long)ceil_div(prm.n_q, 64) * prm.heads_q * prm.batch < multiprocessors()) return launch_window_ref_m<T, D, 32>(prm, st);
   return launch_window_ref_m<T, D, 64>(prm, st);
 }
 
