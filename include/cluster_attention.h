@@ -410,7 +410,8 @@ int ca_attn_recomputed(const void* ws);
 
 /* Diagnostic hook for tests of the failure path (process-wide, not thread-safe; affects the
  * attention calls issued after it).  wait_limit_cycles: SM cycles after which a device-side wait
- * of the tensor-core attention kernel gives up (<= 0 restores the default of about two seconds).
+ * of the tensor-core attention kernels (clusters, bf16 windows) gives up (<= 0 restores the default of about
+ * two seconds).
  * skip_key_load: counted in 64 keys from the start of a CTA's walk over its query tiles; the loader
  * of every CTA leaves out the key rows of the step of 128 keys that holds these, so that the waits for
  * them run out: the kernel records CA_ERR_TIMEOUT, releases its tensor memory and returns, and the

@@ -1173,6 +1173,7 @@ void attn_tc_set_debug(long long wait_limit_cycles, int skip_key_load) {
   g_wait_limit = wait_limit_cycles > 0 ? wait_limit_cycles : kWaitLimitCycles;
   g_skip_key_load = skip_key_load;
 }
+DebugWait debug_wait() { return DebugWait{g_wait_limit, g_skip_key_load}; }
 
 int launch_attn_tc(const ca_problem_t& pr, const void* Qp, const void* Kp, const void* Vp, const float* ck,
                    const float* cv, const int32_t* count_k, const int32_t* block_idx, const int32_t* keep_count,

@@ -144,5 +144,10 @@ int launch_attn_tc(const ca_problem_t& pr, const void* Qp, const void* Kp, const
                    LaunchStream st);
 // diagnostic hook of the attention kernel (see ca_debug_attn_wait in the public header)
 void attn_tc_set_debug(long long wait_limit_cycles, int skip_key_load);
+struct DebugWait {
+  long long limit;               // cycles after which a wait gives up
+  int skip_key_load;             // the step of 64 keys that the loaders leave out, -1: none
+};
+DebugWait debug_wait();          // (the window kernel's waits go by it too)
 
 }  // namespace ca

@@ -80,6 +80,7 @@ struct WtParams {
   int blocks, rows_first;                  // blocks of a head; order of the pieces
   long long wait_limit;
   int wide;                                // rows of O start at 32-byte boundaries
+  int skip_key_load;                       // diagnostic hook: the loader leaves out the keys of the step with these 64 (-1: none)
 };
 
 __device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map, int x, int y, int z, int w, uint32_t bar) {
@@ -300,10 +301,12 @@ window_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
           queries(0);
           if (!ok) break;
           if (steps >= C::NK && !relaxed(b_k_empty(k_slot), k_ph)) { ok = false; break; }
-          mbar_expect_tx(b_k_full(k_slot), C::TILE_BYTES);
+          if (steps != (prm.skip_key_load >> 1)) {           // diagnostic: this slot never fills, its waiters time out
+            mbar_expect_tx(b_k_full(k_slot), C::TILE_BYTES);
 #pragma unroll
-          for (int pn = 0; pn < C::PANELS; ++pn)
-            tma_load_4d(s_k + k_slot * C::TILE_BYTES + pn * C::PANEL_BYTES, &tm_k, pn * 64, t * kWtKeys, g, w.b, b_k_full(k_slot));
+            for (int pn = 0; pn < C::PANELS; ++pn)
+              tma_load_4d(s_k + k_slot * C::TILE_BYTES + pn * C::PANEL_BYTES, &tm_k, pn * 64, t * kWtKeys, g, w.b, b_k_full(k_slot));
+          }
           if (++k_slot == C::NK) { k_slot = 0; k_ph ^= 1; }
           queries(1);
           if (!ok) break;
@@ -727,7 +730,9 @@ int launch_window_tc(WindowParams& w, int D, LaunchStream st) {
   const double reach = (w.left < 0 ? w.n_k : fmin((double)w.n_k, (double)w.left + (w.right < 0 ? w.n_k : w.right) + 2.0 * kWtRows));
   prm.rows_first = (double)w.batch * w.heads_kv * reach * D * 4 < 80e6;
   // A wait for the next piece can be as long as a piece: 20 us for every step of one, which takes 2, on top of the usual limit.
-  prm.wait_limit = kWaitLimitCycles + (long long)(fmin(reach + w.sinks, (double)w.n_k) / kWtKeys + 4) * 40000;
+  const DebugWait debug = debug_wait();
+  prm.skip_key_load = debug.skip_key_load;
+  prm.wait_limit = debug.limit + (long long)(fmin(reach + w.sinks, (double)w.n_k) / kWtKeys + 4) * 40000;
   prm.wide = (reinterpret_cast<uintptr_t>(w.o) % 32 == 0) && (w.batch == 1 || w.o_b % 16 == 0) && (w.heads_q == 1 || w.o_h % 16 == 0) &&
              (w.n_q == 1 || w.o_n % 16 == 0);
   const int sms = multiprocessors();
