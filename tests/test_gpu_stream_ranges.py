@@ -68,7 +68,7 @@ def steps(n, B, H, G, d, dtype, logits):
 @pytest.mark.parametrize("way", WAYS)
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("H,G", [(2, 2), (6, 1)])
-@pytest.mark.parametrize("size", [1e-35, 1e-33, 1e-30, 1.0, 1e30, 1e36])
+@pytest.mark.parametrize("size", [3e-42, 1e-40, 1e-38, 1e-35, 1e-33, 1e-30, 1.0, 1e30, 1e36])
 @pytest.mark.parametrize("n", [5, 40, 700])
 def test_values_of_any_size(way, d, H, G, size, n):
     """Their weighted mean is as accurate at the ends of the range as in the middle; few of the rows have most of the weight."""
