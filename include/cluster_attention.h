@@ -358,6 +358,7 @@ int cache_append(const ca_cache_t* c, int32_t n, const ca_rows_t* K, const ca_ro
  *   j >= N - 1 - left   or   j < sinks
  * are visible.  O [batch, heads_q, 1, head_dim] = softmax-weighted mean of their values, lse
  * [batch, heads_q] fp32 or NULL = log-sum-exp of their logits; without a visible row zeros and -inf.
+ * O may be Q, with the same strides, and overlaps nothing else of the call.
  * What is not visible is not read.  A length out of range is cut to the range, a page out of range read as zero
  * keys and values, and CA_ERR_BAD_INDEX recorded (also where the last append on this workspace recorded it).  The result does not depend on how the GPU schedules the parts.
  */

@@ -659,6 +659,7 @@ int paged_attention_fwd(const ca_cache_t* c, const ca_rows_t* Q, const void* K_p
   if (!lengths || !page_table || appended < 0) return CA_ERR_INVALID_ARG;
   CA_TRY(check_rows(Q, c->batch, c->heads_q, 1, c->head_dim, c->dtype, false));
   CA_TRY(check_rows(O, c->batch, c->heads_q, 1, c->head_dim, c->dtype, true));
+  if (Q->data == O->data && !same_strides(Q, O, c->batch, c->heads_q, 1)) return CA_ERR_INVALID_ARG;
   if (!K_pages || !V_pages || !aligned16(K_pages) || !aligned16(V_pages)) return CA_ERR_INVALID_ARG;
   if (!ws || !aligned16(ws) || ws_bytes < paged_workspace_bytes(*c)) return CA_ERR_WORKSPACE;
   return launch_paged(*c, Q, K_pages, V_pages, lengths, appended, page_table, scale_of(c->softmax_scale, c->head_dim), O, lse, ws,

@@ -169,3 +169,24 @@ def test_largest_values_inside_a_window(way, left, sinks):
     O, lse = ask(way, q, k, v, LOG2, left, sinks)
     assert torch.isfinite(O).all()
     check(way, q, torch.nan_to_num(k), clean, LOG2, 1, (O, lse), "a window", left, sinks)
+
+
+@pytest.mark.parametrize("way", [w for w in WAYS if w[0] == "cache"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("group", [1, 3, 8, 20])
+def test_an_output_in_the_place_of_the_queries(way, d, group):
+    """Sums that are taken again read the queries again, before their place is written."""
+    g = generator(group)
+    n, dt = 700, DT[way[1]]
+    per = -(-n // 16) + way[2]
+    cache = binding.PagedCache(binding.make_cache_problem(3, 2 * group, 2, d, way[1], 16, 3 * per, per), DEV,
+                               page_table=torch.arange(3 * per, device=DEV).reshape(3, per).int())
+    cache.lengths.copy_(torch.tensor([n, 3, 40]))
+    for pool in (cache.K_pages, cache.V_pages):
+        pool.copy_(torch.randn(pool.shape, generator=g, device=DEV).to(dt))
+    cache.V_pages[..., 5] = torch.finfo(dt).max
+    q = torch.randn((3, 2 * group, 1, d), generator=g, device=DEV).to(dt)
+    want = [x.clone() for x in cache.paged_attention_fwd(q)]
+    assert torch.isfinite(want[0].float()).all()
+    got = cache.paged_attention_fwd(q, out=q)
+    assert got[0] is q and torch.equal(q, want[0]) and torch.equal(got[1], want[1])

@@ -1,7 +1,7 @@
 """Arguments of the binding that are refused on the host."""
 import pytest
 
-from paper_2608_26965_b200 import binding
+from paper_2608_26965_b200 import binding, build
 
 
 @pytest.mark.parametrize("big", [2 ** 31, 2 ** 32, 2 ** 32 + 5, 2 ** 63 - 1, -2 ** 31 - 1, -2 ** 32])
@@ -30,3 +30,13 @@ def test_positions_without_rotary_are_refused():
             plan.forward(None, None, None, **args)
         with pytest.raises(binding.ClusterAttnError, match="positions without rotary"):
             plan.forward_adaptive(None, None, None, 0.5, **args)
+
+
+def test_an_output_that_is_the_queries_keeps_their_strides():
+    build.build()
+    lib = binding.load_library()
+    cache = binding.make_cache_problem(batch=2, heads_q=8, heads_kv=2, head_dim=128, dtype="bf16", page_rows=16, pages=100, pages_per_sequence=20)
+    at = 1 << 20                                            # (an address that nothing reads: the calls are refused)
+    q = binding.CaRows(at, 1 << 16, 1 << 12, 128)
+    for other in (binding.CaRows(at, 1 << 17, 1 << 12, 128), binding.CaRows(at, 1 << 16, 1 << 11, 128)):
+        assert lib.paged_attention_fwd(cache, q, at, at, at, 0, at, other, None, at, 1 << 30, None) == 1
