@@ -378,7 +378,9 @@ int paged_attention_fwd(const ca_cache_t* c, const ca_rows_t* Q, const void* K_p
  * bf16 storage runs on tcgen05 tensor cores with fp32 accumulation and bf16 probabilities, fp32 storage on
  * products of tf32 halves with the accuracy of fp32; CA_ATTN_FP32 in flags selects the FP32 CUDA-core kernel,
  * and it computes again what a tensor core gives as not finite, so that masked values may be anything.  A
- * length out of range is cut to it and CA_ERR_BAD_INDEX recorded.
+ * length out of range is cut to it and CA_ERR_BAD_INDEX recorded.  Strides of zero in Q, K or V are allowed, but take
+ * bf16 storage to the CUDA-core kernel, some ten times slower; so do, row by row, visible numbers that are
+ * infinite or NaN.
  */
 typedef struct {
   int32_t batch, heads_q, heads_kv;

@@ -7,7 +7,7 @@
 // (the tcgen05 tiles have 64 rows and more, nine tenths of them empty here, and the tensor core is not what is waited for).
 // A warp's step is a chain of products, softmax and products: it is the length of that chain, and how many warps are on it, that
 // costs bandwidth before memory does (with the query heads as the 16 rows of the product, half of them empty, 623 instructions a
-// step: two sequences of 131,000 rows, 40 heads, 981 us; as its 8 columns 786, 6.8 TB/s).
+// step: two sequences of 131,000 rows, 40 heads, 981 us; as its 8 columns 790, 6.8 TB/s).
 //
 // Split: the visible rows of all sequences and key heads are one line of units, which the CTAs cut into equal
 // parts: whatever the lengths, every CTA has as much to do as any other.  A part begins and ends anywhere; where a sequence's rows lie in
@@ -532,9 +532,9 @@ __device__ __forceinline__ float4 replaced(float4 mean, float4 small, float l) {
   return mean;
 }
 // Sums of weighted small values of a query head, by a warp: of the visible rows, 32 at a time, groups first, first + step, ... .  A lane
-// weighs one of the 32, then has columns lane D / 32 and the next.  Slow, and called for sums beyond fp32
-// and values in sight that are infinite or NaN alone: with a NaN in each sequence, 64 of up to 8,192 rows, 8 key heads of 4 query heads, take
-// 1.5 ms instead of 0.05, two of 131,000 rows, 40 heads, 7.2 instead of 0.8.
+// weighs one of the 32, then has columns lane D / 32 and the next.  Slow, and called only for sums beyond fp32 and where values in sight are
+// infinite or NaN: with a NaN in each sequence, 64 of up to 8,192 rows, 8 key heads of 4 query heads, take 1.5 ms instead of 0.05, two of 131,000
+// rows, 40 heads, 7.2 instead of 0.8.
 template <typename T, int D>
 __device__ __noinline__ float4 small_sums(const PagedParams& prm, int b, int h, int head, float m, int first, int step) {
   const int lane = threadIdx.x & 31;

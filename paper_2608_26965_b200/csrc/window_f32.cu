@@ -3,14 +3,15 @@
 // tf32 has 11 significant bits, so each operand is split in two, x = hi + lo with hi = x rounded to tf32 and lo = the rest cut
 // to tf32, and a product is lo hi + hi lo + hi hi: what is left out is 2^-22 of it.  The tensor core cuts its sums instead of rounding
 // them, which over long chains loses more than that (2.7e-6 of the result with one accumulator for all); so chains of upper parts are two
-// products long and are added up in fp32, and the small products have chains of their own: 3.4e-7 off where a plain fp32 form is
-// 5.5e-7 (12 heads of 1,370 rows, d = 64, 148 rows to either side).
+// products long and are added up in fp32, and the small products have chains of their own: 3.2e-7 off where a plain fp32 form is
+// 6.3e-7 (12 heads of 1,370 rows, d = 64, 148 rows to either side).
 //
 // Three products for one, at four times the rate of the CUDA cores' multiply-adds, and the operands come from shared memory a
-// word per lane and product: the 1,370 rows take 47 us (window_ref.cu, which waits for vectors of shared memory, 73), 2 x 8 heads of 4,000
-// rows, causal, d = 64, 500 rows before 229 us (331).  What bounds it is the chain of a warp's step (copy to registers, split,
-// product, softmax, product): tensor pipe 43 % busy, an instruction every third cycle, with the eight warps that 255 registers allow (168
-// registers and twelve warps: 55 us, 128 and sixteen: 76, for the registers that then go through memory).
+// word per lane and product: the 1,370 rows take 48 us (window_ref.cu, which waits for vectors of shared memory, 80), 2 x 8 heads of 4,000
+// rows, causal, d = 64, 500 rows before 221 us (351).  What bounds it is the chain of a warp's step (copy to registers, split,
+// product, softmax, product): tensor pipe 43 % busy, an instruction every other cycle, with the eight warps that 255 registers allow (168
+// registers and twelve warps: 55 us, 128 and sixteen: 76, for the registers that then go through memory).  Each of the four warps splits
+// the tiles by itself, and the queries in every tile again; tf32 products of tcgen05 are not used.
 //
 // A warp has 16 query rows in registers, a CTA four warps; keys and values come 32 at a time by asynchronous copies, shared by the
 // warps, while the 32 before are worked on.
@@ -18,7 +19,8 @@
 //     O += P V       P as it is held: its keys 2 t and 2 t + 1 stand at columns t and t + 4 of the product, and V's rows likewise
 // Masked probabilities are 0, and 0 x infinity is not: rows whose result is not finite are marked and computed again by the
 // CUDA-core kernel (as those of the bf16 kernel are).  So are rows with a result below 2^-100 that is not zero: of a value below some 2^-112
-// the lower half is below the normal range, where tf32 has only ten bits behind 2^-126.
+// the lower half is below the normal range, where tf32 has only ten bits behind 2^-126.  (Scores lose as much where queries below 2^-116
+// meet keys above 2^116, or keys such queries.)
 #include <math.h>
 
 #include "tc_ptx.cuh"

@@ -5,9 +5,9 @@
 // storage).  A thread has R x 4 scores and R x D/8 columns of the result in registers.  What bounds it is reading shared memory, not the
 // multiply-adds (two to an instruction): a vector of 16 bytes per lane takes 3.6 cycles whether lanes read the same
 // one or not, so 8 vectors for 32 instructions (R = 4) keep the reads of four warps at it for 115 cycles and the multiply-adds
-// for 64.  2 x 8 heads of 4,000 rows, causal, d = 128: 2.08 ms, 31 TFLOP/s of visible pairs (R = 2 2.93 ms; R = 8 3.19, for want of
+// for 64.  2 x 8 heads of 4,000 rows, causal, d = 128: 2.2 ms, 30 TFLOP/s of visible pairs (R = 2 2.9 ms; R = 8 3.2, for want of
 // registers and warps).  M = 64 with R = 4; M = 32 with R = 2 where tiles of 64 rows would be fewer than one to an SM (100 rows, one
-// head: 10.4 us instead of 15.4).
+// head, fp32: 11.8 us instead of 20.9 at d = 64, 19.3 instead of 29.4 at d = 128; 12 heads of 400 rows 38.8 instead of 46.4).
 // Only tiles at a border of the window are masked: what a row does not see takes no part, whatever stands there
 // (0 x infinity would).  Rows with a mean that is not finite are gone over a second time, with small values (kernels.h).
 #include <math.h>

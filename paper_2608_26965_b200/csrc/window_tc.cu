@@ -17,12 +17,12 @@
 // 0 x infinity is not: rows whose result is not finite are marked and computed again on the CUDA cores, where
 // what is masked takes no part and no P is above 1 (a launch of its own, which ends at once when no row is marked).
 //
-// What bounds it: a step (256 x 128 scores, d = 128) takes some 3,200 cycles.  The products take 2,650 of them, 2,048 if shared
+// What bounds it: a step (256 x 128 scores, d = 128) takes some 3,100 cycles.  The products take 2,650 of them, 2,048 if shared
 // memory fed both operands of Q K^T without a pause (they need all of its 128 bytes a cycle, and the loads of the next tiles and V
 // come on top); the exponentials 1,900 of the special-function unit's time.  Between the two lies the chain S -> P -> O of each
 // query tile.  Calls in a row are bound by power: 40 heads of 32,760 rows, d = 128, two frames of 1,560 to either side and the first
-// one take 4.01 ms by themselves and 4.62 in a row (1.06 PFLOP/s of visible pairs, 1.19 with the masked parts of tiles; plain
-// products of 8,192^3 1.41 in a row).  Tried and slower: 16 softmax warps with half of a row's columns each (4.40 ms), the
+// one take 4.1 ms by themselves and 4.6 in a row (1.07 PFLOP/s of visible pairs, 1.20 with the masked parts of tiles; plain
+// products of 8,192^3 1.41 in a row).  384 threads leave 168 registers to each, of which 68 bytes go by way of local memory.  Tried and slower: 16 softmax warps with half of a row's columns each (4.40 ms), the
 // issuing thread looking at barriers without a pause (5.27: its looks delay everybody's), a pass for the exact maximum (4.17),
 // every eighth instead of every sixteenth pair of exponentials on the FMA units (4.26; none 4.09, but 476 us instead of 452 at d = 64,
 // 8 heads of 18,944 rows), P handed over in halves (4.07) or in whole (4.19), steps of 64 keys with two score buffers to a query tile
